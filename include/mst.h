@@ -28,6 +28,7 @@
 #ifndef MST_H_
 #define MST_H_
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -205,6 +206,106 @@ mst_status_t mst_strided_attention_bwd(const void* Q, const void* K, const void*
                                        int32_t seq_len, int32_t heads, int32_t head_dim, int32_t stride, void* dQ,
                                        void* dK, void* dV, int64_t ldg, mst_stream_t stream);
 
+/* Norm of queries and keys for each head with the position rotation in the same pass: what may stand between the fused qkv
+ * activation and the attention.  For a head's row x of D = head_dim values at position p
+ *   n = gamma . x / sqrt(mean(x^2) + eps)          (gamma NULL: n = x, rotation only)
+ *   y = n with the pairs (a, b) among its first rot_dim values turned by the angles p * inv_freq[i], i < rot_dim / 2:
+ *       a' = a cos - b sin,  b' = a sin + b cos;   pair i is (i, i + rot_dim / 2), or (2i, 2i + 1) where `interleaved` is set.
+ *   head_dim     a multiple of 8 up to 256
+ *   rot_dim      a multiple of 16 up to head_dim; 0: no rotation (inv_freq may be NULL)
+ *   inv_freq     device float [rot_dim / 2], in radians per position
+ *   gamma_q, gamma_k   device float [head_dim], each NULL or 16-byte aligned; eps >= 0
+ * Sums, norms and the turn are fp32, an angle is formed and reduced in fp64 (positions far out keep it to 2e-7); one rounding, at
+ * the end. */
+typedef struct {
+  int32_t head_dim, rot_dim, interleaved;
+  float eps;
+  const float* inv_freq;
+  const float* gamma_q;
+  const float* gamma_k;
+} mst_rotation_t;
+
+/* Q_out, K_out = norm and rotation of Q, K.  Rows of `ld` (out: `ldo`) elements, one a token, heads_q (heads_k) heads side by side
+ * from Q (K) on, so the column slices of a fused activation can be passed as they are; either count may be 0 (its pointers are
+ * then ignored).  positions: device int32 [tokens], or NULL: token t is at position t mod seq_len.  dtype of Q, K and the results: MST_F32
+ * or MST_BF16.  Pointers 16-byte aligned, ld and ldo multiples of 8, otherwise MST_ERR_SHAPE.  In place (Q_out == Q, K_out == K, ldo ==
+ * ld) is allowed; other overlaps are not.
+ * This call and the next four take pointers of the current device only: any other (of the host, of another device) is
+ * MST_ERR_INVALID_ARG, before anything is launched.  They keep nothing between calls and have no scratch of their own, so calls on
+ * different streams, captured ones too, may overlap as long as their outputs and workspaces are different ones. */
+mst_status_t mst_qk_norm_rotate_fwd(const mst_rotation_t* rotation, mst_dtype_t dtype, int64_t tokens, int32_t seq_len,
+                                    const int32_t* positions, int32_t heads_q, int32_t heads_k, const void* Q, const void* K,
+                                    int64_t ld, void* Q_out, void* K_out, int64_t ldo, mst_stream_t stream);
+
+/* Gradients of mst_qk_norm_rotate_fwd.  Q, K, ld: its inputs; dQ_out, dK_out, lddo: upstream gradients.  With z the upstream row
+ * turned back, r = 1 / sqrt(mean(x^2) + eps), u = z . gamma:
+ *   dx = r (u - x r^2 mean(u . x)),   dgamma = sum over tokens and heads of z . x r      (gamma NULL: dx = z)
+ * dQ, dK (rows of ldg elements) may be dQ_out, dK_out or Q, K themselves with the same leading dimension.  dgamma_q, dgamma_k:
+ * device float [head_dim], written, not added to; NULL to skip (must be NULL where gamma is).  fp32 sums in a fixed order, no
+ * atomics: results repeat bit for bit.
+ * workspace: device, 16-byte aligned, at least mst_qk_norm_rotate_bwd_workspace bytes (MST_ERR_CAPACITY otherwise; may be NULL with neither
+ * dgamma), contents irrelevant before and after the call. */
+mst_status_t mst_qk_norm_rotate_bwd(const mst_rotation_t* rotation, mst_dtype_t dtype, int64_t tokens, int32_t seq_len,
+                                    const int32_t* positions, int32_t heads_q, int32_t heads_k, const void* Q, const void* K,
+                                    int64_t ld, const void* dQ_out, const void* dK_out, int64_t lddo, void* dQ, void* dK,
+                                    int64_t ldg, float* dgamma_q, float* dgamma_k, void* workspace, size_t workspace_bytes,
+                                    mst_stream_t stream);
+mst_status_t mst_qk_norm_rotate_bwd_workspace(const mst_rotation_t* rotation, int64_t tokens, size_t* bytes);
+
+/* A cache of keys and values in pages of page_size tokens, bf16.  Value d of key head h of the token in slot s of page p is at
+ * K[p * page_stride + s * token_stride + h * head_stride + d], V the same: strides in elements, multiples of 8, pointers 16-byte
+ * aligned. */
+typedef struct {
+  void* K;
+  void* V;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t num_pages, page_size, kv_heads, head_dim;
+} mst_paged_cache_t;
+
+/* The sequences of one step.  Sequence b has rows first[b] .. first[b + 1] - 1 of the token-major activations as its new tokens (none
+ * is allowed) and holds len[b] tokens with them: the new ones are at its last positions, position p in slot p mod page_size of
+ * page page_table[b * table_stride + p / page_size].
+ *   first        device int32 [batch + 1], ascending
+ *   len          device int32 [batch]
+ *   page_table   device int32 [batch x table_stride]; entries of pages that a length does not reach are not read
+ *   tokens       rows of the activations; rows from first[batch] on belong to no sequence: outputs there are left as they were
+ *   max_new, max_len   about the largest count of new tokens and the largest length: they decide how the work is cut up, so they go into
+ *                speed and the order of sums; every length is served whatever they say
+ * first, len and the table live on the device and are checked there: a token at a negative position (len[b] below its new tokens)
+ * attends to nothing, and an append passes it over; a page entry outside [0, num_pages), or a position at or beyond table_stride * page_size, is
+ * left out (not written, not attended to) and sets bit 4 of mst_device_error_flags. */
+typedef struct {
+  int32_t batch, tokens, max_new, max_len;
+  const int32_t* first;
+  const int32_t* len;
+  const int32_t* page_table;
+  int32_t table_stride;
+} mst_paged_batch_t;
+
+/* The new tokens' keys, normed and rotated by their positions (mst_rotation_t; NULL: as they are), and values into the cache, and the
+ * queries, normed and rotated, into Q_out, in one launch.  Q, K, V: device bf16, rows of `ld` elements (slices of a fused activation);
+ * Q and Q_out (rows of ldq elements) may be NULL, heads_q is then ignored, or the same with ldq == ld.  Two tokens that name one slot leave
+ * either's row. */
+mst_status_t mst_paged_append(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, const mst_rotation_t* rotation,
+                              int32_t heads_q, const void* Q, const void* K, const void* V, int64_t ld, void* Q_out, int64_t ldq,
+                              mst_stream_t stream);
+
+/* Attention of the new tokens over the cache (their own keys and values included: append first), the serving form of
+ * mst_strided_attention_fwd: with i the query's position
+ *   Out = sum_{j in S_i} softmax_j(q . k_j / sqrt(d)) v_j,   S_i = { j <= i : i - j < l  or  (i - j) mod l == 0 },
+ * l = stride; from the longest length on every earlier position is attended.  heads is a multiple of kv_heads: query head h reads key
+ * head h / (heads / kv_heads).  Q: device bf16, rows of ldq elements; Out: device bf16, rows of ldo elements; lse: device float [heads x tokens]
+ * or NULL, log sum_j exp(q . k_j / sqrt(d)).  A query without keys gets Out = 0 and lse = -inf.  What S_i leaves out does not reach
+ * a result, be it infinite or NaN.  Scores and sums are fp32, the softmax weights are rounded to bf16 before they multiply the values.
+ * Supported: head_dim 64 or 128, any positive stride, ldq and ldo multiples of 8, 16-byte aligned pointers; anything else MST_ERR_SHAPE.  No atomics on results: they repeat bit for bit for the same arguments.
+ * workspace: device, 16-byte aligned, at least mst_paged_attention_workspace bytes (MST_ERR_CAPACITY otherwise; NULL where that is 0),
+ * contents irrelevant before and after the call. */
+mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, int32_t heads, int32_t stride,
+                                 const void* Q, int64_t ldq, void* Out, int64_t ldo, float* lse, void* workspace,
+                                 size_t workspace_bytes, mst_stream_t stream);
+mst_status_t mst_paged_attention_workspace(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, int32_t heads,
+                                           int32_t stride, size_t* bytes);
+
 /* Weight gradient on the mask only, dW[k] = sum_t dY[t,o_k] X[t,i_k] for the k-th active entry in CSR order
  * (same passage).  dW_vals device float [nnz].  May use the per-device split scratch (see the conventions above). */
 mst_status_t mst_sddmm_dw(const mst_layer_t* layer, const void* dY, int64_t lddy, const void* X, int64_t ldx, int64_t T,
@@ -324,7 +425,8 @@ mst_status_t mst_er_densities(int32_t n_layers, const int32_t* out_features, con
 /* Sticky error bits of kernels that run without a layer handle (bit 0: a bounded wait inside the tensor-core
  * contraction expired and the block gave up; its output is then undefined; bit 1: the same in the attention
  * kernel; bit 2: the same in the structured-sparse contraction;
- * bit 3: the same in the CUDA-core SpMM / SDDMM).  Synchronises the device. */
+ * bit 3: the same in the CUDA-core SpMM / SDDMM; bit 4: a page of a cache that does not exist was named, see mst_paged_batch_t,
+ * since the last call of this function, which clears it; bit 5: a bounded wait inside the paged attention expired).  Synchronises the device. */
 mst_status_t mst_device_error_flags(int32_t* flags);
 
 /* The same step without the final wait: inputs are copied on a copy-in stream owned by the layer, the three products

@@ -24,7 +24,8 @@ STATUS_NAMES = {0: "MST_OK", 1: "MST_ERR_INVALID_ARG", 2: "MST_ERR_SHAPE", 3: "M
                 5: "MST_ERR_INFEASIBLE", 6: "MST_ERR_NONFINITE", 7: "MST_ERR_CORRUPT", 8: "MST_ERR_CUDA",
                 9: "MST_ERR_NOT_PACKED"}
 EXPORTS = ["mst_layer_create", "mst_layer_destroy", "mst_set_compute_path", "mst_layer_path_in_use", "mst_launch_count", "mst_track_values", "mst_values_changed", "mst_layer_nnz", "mst_pack", "mst_export_csr", "mst_export_csc",
-           "mst_values", "mst_validate", "mst_spmm_fwd", "mst_spmm_bwd_x", "mst_spmm_fwd_gelu", "mst_spmm_bwd_x_gelu", "mst_strided_attention_fwd", "mst_strided_attention_bwd", "mst_sddmm_dw", "mst_dense_grad", "mst_sddmm_from_dense", "mst_dense_grad_dw",
+           "mst_values", "mst_validate", "mst_spmm_fwd", "mst_spmm_bwd_x", "mst_spmm_fwd_gelu", "mst_spmm_bwd_x_gelu", "mst_strided_attention_fwd", "mst_strided_attention_bwd", "mst_qk_norm_rotate_fwd", "mst_qk_norm_rotate_bwd", "mst_qk_norm_rotate_bwd_workspace",
+           "mst_paged_append", "mst_paged_attention", "mst_paged_attention_workspace", "mst_sddmm_dw", "mst_dense_grad", "mst_sddmm_from_dense", "mst_dense_grad_dw",
            "mst_update_counts", "mst_rand_bracket", "mst_topology_update", "mst_topology_update_many", "mst_layer_step_host", "mst_layer_step_host_async", "mst_layer_step_host_wait", "mst_mask_to_csr_noalloc",
            "mst_device_error_flags", "mst_sv_sparsity", "mst_sv_update_fraction", "mst_er_densities",
            "mst_status_string"]
@@ -51,6 +52,52 @@ class SvSchedule(ctypes.Structure):
         super().__init__(max_sparsity, n_stages, delta_w, t_ultra, delta_r)
 
 
+class Rotation(ctypes.Structure):
+    """Norm of each head and rotation by position: ``inv_freq`` fp32 [rot_dim / 2], ``gamma_q``, ``gamma_k`` fp32 [head_dim] or None
+    (that side is rotated only); device tensors, kept alive by this object."""
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p), ("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p)]
+
+    def __init__(self, head_dim: int, rot_dim: int, inv_freq=None, gamma_q=None, gamma_k=None, eps: float = 1e-6,
+                 interleaved: bool = False):
+        super().__init__(head_dim, rot_dim, int(bool(interleaved)), eps, _ptr(inv_freq) or None, _ptr(gamma_q), _ptr(gamma_k))
+        self.tensors = (inv_freq, gamma_q, gamma_k)
+
+
+class PagedCache(ctypes.Structure):
+    """Keys and values in pages: two bf16 tensors [num_pages, page_size, kv_heads, head_dim] of the same strides, the last of them 1 (a
+    transposed view of [num_pages, kv_heads, page_size, head_dim] will do); kept alive by this object."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+    def __init__(self, K, V):
+        if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride() or K.stride(3) != 1:
+            raise ValueError("K and V: [num_pages, page_size, kv_heads, head_dim] with equal strides, 1 between the values of a row")
+        if str(K.dtype) != "torch.bfloat16" or str(V.dtype) != "torch.bfloat16":
+            raise ValueError("K and V hold bfloat16")
+        super().__init__(K.data_ptr(), V.data_ptr(), K.stride(0), K.stride(1), K.stride(2), *K.shape)
+        self.tensors = (K, V)
+
+
+class PagedBatch(ctypes.Structure):
+    """The sequences of one step: ``first`` int32 [batch + 1], ``length`` int32 [batch], ``page_table`` int32 [batch, pages], ``tokens``
+    rows of the activations, ``max_new`` and ``max_len`` about the largest count of new tokens and the largest length (speed only);
+    device tensors, kept alive by this object."""
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("first", ctypes.c_void_p), ("len", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int32)]
+
+    def __init__(self, first, length, page_table, tokens: int, max_new: int, max_len: int):
+        for t, dims in ((first, 1), (length, 1), (page_table, 2)):
+            if t.dim() != dims or str(t.dtype) != "torch.int32" or not t.is_contiguous():
+                raise ValueError("first [batch + 1], length [batch] and page_table [batch, pages] are contiguous int32 tensors")
+        if first.shape[0] != length.shape[0] + 1 or page_table.shape[0] != length.shape[0]:
+            raise ValueError("first, length and page_table disagree on the number of sequences")
+        super().__init__(length.shape[0], tokens, max_new, max_len, first.data_ptr(), length.data_ptr(), page_table.data_ptr() or None,
+                         page_table.shape[1])
+        self.tensors = (first, length, page_table)
+
+
 class UpdateStats(ctypes.Structure):
     _fields_ = [("nnz_before", ctypes.c_int64), ("nnz_after", ctypes.c_int64), ("n_prune", ctypes.c_int64),
                 ("n_grad", ctypes.c_int64), ("n_rand", ctypes.c_int64), ("max_row_nnz", ctypes.c_int64)]
@@ -62,6 +109,7 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 _vp, _i32, _i64, _f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
+_size = ctypes.c_size_t
 _sig = {
     "mst_layer_create": [ctypes.POINTER(_vp), _i32, _i32, _i32, ctypes.c_int, _i64],
     "mst_layer_destroy": [_vp],
@@ -83,6 +131,14 @@ _sig = {
     "mst_strided_attention_fwd": [_vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp],
     "mst_strided_attention_bwd": [_vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp,
                                   _i64, _vp],
+    "mst_qk_norm_rotate_fwd": [ctypes.POINTER(Rotation), ctypes.c_int, _i64, _i32, _vp, _i32, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _vp],
+    "mst_qk_norm_rotate_bwd": [ctypes.POINTER(Rotation), ctypes.c_int, _i64, _i32, _vp, _i32, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp,
+                               _i64, _vp, _vp, _vp, _size, _vp],
+    "mst_qk_norm_rotate_bwd_workspace": [ctypes.POINTER(Rotation), _i64, ctypes.POINTER(_size)],
+    "mst_paged_append": [ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch), ctypes.POINTER(Rotation), _i32, _vp, _vp, _vp, _i64, _vp,
+                         _i64, _vp],
+    "mst_paged_attention": [ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch), _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _size, _vp],
+    "mst_paged_attention_workspace": [ctypes.POINTER(PagedCache), ctypes.POINTER(PagedBatch), _i32, _i32, ctypes.POINTER(_size)],
     "mst_sddmm_dw": [_vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp],
     "mst_dense_grad": [_vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_int, _vp, _vp],
     "mst_sddmm_from_dense": [_vp, _vp, _vp, _vp],
@@ -256,6 +312,50 @@ def mst_strided_attention_bwd(Q, K, V, ld: int, Out, ldo: int, dOut, lddo: int, 
     _check(_lib.mst_strided_attention_bwd(_ptr(Q), _ptr(K), _ptr(V), ld, _ptr(Out), ldo, _ptr(dOut), lddo, _ptr(lse), batch,
                                           seq_len, heads, head_dim, stride, _ptr(dQ), _ptr(dK), _ptr(dV), ldg,
                                           _stream(stream)), "mst_strided_attention_bwd")
+
+
+def _bytes(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def mst_qk_norm_rotate_fwd(rotation: Rotation, dtype: int, tokens: int, seq_len: int, positions, heads_q: int, heads_k: int, Q, K,
+                           ld: int, Q_out, K_out, ldo: int, stream=None) -> None:
+    _check(_lib.mst_qk_norm_rotate_fwd(rotation, dtype, tokens, seq_len, _ptr(positions), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
+                                       _ptr(Q_out), _ptr(K_out), ldo, _stream(stream)), "mst_qk_norm_rotate_fwd")
+
+
+def mst_qk_norm_rotate_bwd_workspace(rotation: Rotation, tokens: int) -> int:
+    n = _size()
+    _check(_lib.mst_qk_norm_rotate_bwd_workspace(rotation, tokens, ctypes.byref(n)), "mst_qk_norm_rotate_bwd_workspace")
+    return n.value
+
+
+def mst_qk_norm_rotate_bwd(rotation: Rotation, dtype: int, tokens: int, seq_len: int, positions, heads_q: int, heads_k: int, Q, K,
+                           ld: int, dQ_out, dK_out, lddo: int, dQ, dK, ldg: int, dgamma_q=None, dgamma_k=None, workspace=None,
+                           stream=None) -> None:
+    """workspace: a tensor of at least ``mst_qk_norm_rotate_bwd_workspace`` bytes."""
+    _check(_lib.mst_qk_norm_rotate_bwd(rotation, dtype, tokens, seq_len, _ptr(positions), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
+                                       _ptr(dQ_out), _ptr(dK_out), lddo, _ptr(dQ), _ptr(dK), ldg, _ptr(dgamma_q), _ptr(dgamma_k),
+                                       _ptr(workspace), _bytes(workspace), _stream(stream)), "mst_qk_norm_rotate_bwd")
+
+
+def mst_paged_append(cache: PagedCache, batch: PagedBatch, rotation: Optional[Rotation], heads_q: int, Q, K, V, ld: int, Q_out=None,
+                     ldq: int = 0, stream=None) -> None:
+    _check(_lib.mst_paged_append(cache, batch, rotation, heads_q, _ptr(Q), _ptr(K), _ptr(V), ld, _ptr(Q_out), ldq, _stream(stream)),
+           "mst_paged_append")
+
+
+def mst_paged_attention_workspace(cache: PagedCache, batch: PagedBatch, heads: int, stride: int) -> int:
+    n = _size()
+    _check(_lib.mst_paged_attention_workspace(cache, batch, heads, stride, ctypes.byref(n)), "mst_paged_attention_workspace")
+    return n.value
+
+
+def mst_paged_attention(cache: PagedCache, batch: PagedBatch, heads: int, stride: int, Q, ldq: int, Out, ldo: int, lse=None,
+                        workspace=None, stream=None) -> None:
+    """workspace: a tensor of at least ``mst_paged_attention_workspace`` bytes."""
+    _check(_lib.mst_paged_attention(cache, batch, heads, stride, _ptr(Q), ldq, _ptr(Out), ldo, _ptr(lse), _ptr(workspace),
+                                    _bytes(workspace), _stream(stream)), "mst_paged_attention")
 
 
 def mst_sddmm_dw(layer: int, dY, lddy: int, X, ldx: int, T: int, dW_vals, stream=None) -> None:

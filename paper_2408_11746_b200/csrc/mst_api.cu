@@ -29,6 +29,24 @@ void free_staging(mst_layer* L) {
 
 }  // namespace
 
+mst_status_t mst_on_this_device(std::initializer_list<const void*> pointers) {
+  int dev = 0;
+  MST_CUDA_TRY(cudaGetDevice(&dev));
+  for (const void* p : pointers) {
+    if (!p) continue;
+    cudaPointerAttributes a;
+    const cudaError_t e = cudaPointerGetAttributes(&a, p);
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();      // asked, answered: not left behind for the next call to find
+      if (e == cudaErrorInvalidValue) return MST_ERR_INVALID_ARG;
+      mst_report_cuda_error(e, "cudaPointerGetAttributes", __FILE__, __LINE__);
+      return MST_ERR_CUDA;
+    }
+    if (a.type != cudaMemoryTypeManaged && !(a.type == cudaMemoryTypeDevice && a.device == dev)) return MST_ERR_INVALID_ARG;
+  }
+  return MST_OK;
+}
+
 extern "C" const char* mst_status_string(mst_status_t st) {
   switch (st) {
     case MST_OK: return "ok";

@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cstdio>
 #include <cstdlib>
+#include <initializer_list>
 
 #include "mst.h"
 #include "mst_tc_sparse.cuh"
@@ -184,6 +185,9 @@ struct mst_layer {
   int async_ready;
 };
 
+// MST_OK when every pointer that is not NULL names memory of the current device (or managed memory); about 0.1 us each (mst_api.cu)
+mst_status_t mst_on_this_device(std::initializer_list<const void*> pointers);
+
 static inline size_t mst_elem_size(mst_dtype_t d) { return d == MST_F32 ? 4 : 2; }
 
 // structure (mst_structure.cu)
@@ -228,6 +232,9 @@ mst_status_t mst_split_error_flags(int32_t* flags);
 // sticky error word of the attention kernel's bounded waits (mst_attention.cu)
 mst_status_t mst_attention_error_flags(int32_t* flags);
 mst_status_t mst_attention_bwd_error_flags(int32_t* flags);
+// bit 0: pages that do not exist were named (cleared by this call), bit 1: bounded waits (mst_paged_attention.cu); the append's bit 0 (mst_rotate.cu)
+mst_status_t mst_paged_error_flags(int32_t* flags);
+mst_status_t mst_append_error_flags(int32_t* flags);
 
 // bins of one radix-select pass (digit width MST_SELECT_RADIX_BITS)
 constexpr int MST_SELECT_RADIX_BITS = 11;

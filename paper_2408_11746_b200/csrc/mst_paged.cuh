@@ -1,0 +1,84 @@
+// A cache of keys and values in pages, and the sequences of one step over it: what the append and the attention share.
+// Everything the device is told by device memory (row ranges, lengths, page numbers) is checked there before it becomes an address.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "mst_internal.cuh"
+#include "mst_paged_list.h"
+
+namespace mst_paged {
+
+struct Cache {
+  __nv_bfloat16 *K, *V;
+  int64_t page_stride, token_stride, head_stride;
+  int num_pages, page_size, kv_heads, D;
+};
+struct Batch {
+  const int32_t *first, *len, *table;
+  int batch, tokens, table_stride;
+};
+
+inline mst_status_t check(const mst_paged_cache_t* c, const mst_paged_batch_t* b, Cache* cache, Batch* batch) {
+  if (!c || !b || !c->K || !c->V) return MST_ERR_INVALID_ARG;
+  if (c->num_pages < 0 || c->page_size <= 0 || c->kv_heads <= 0 || c->head_dim <= 0 || b->batch < 0 || b->tokens < 0 || b->table_stride < 0 ||
+      b->max_new < 0 || b->max_len < 0)
+    return MST_ERR_INVALID_ARG;
+  if (b->batch > 0 && (!b->first || !b->len || (!b->page_table && b->table_stride > 0))) return MST_ERR_INVALID_ARG;
+  if (c->kv_heads > 65535 || b->batch > 65535) return MST_ERR_SHAPE;
+  if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->page_stride % 8 != 0 || c->token_stride % 8 != 0 ||
+      c->head_stride % 8 != 0)
+    return MST_ERR_SHAPE;
+  // rows of different slots or heads do not overlap
+  if ((c->page_size > 1 && c->token_stride < c->head_dim) || (c->kv_heads > 1 && c->head_stride < c->head_dim) ||
+      (c->num_pages > 1 && c->page_stride < c->head_dim))
+    return MST_ERR_SHAPE;
+  if (((reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V)) & 15u) != 0 ||
+      ((reinterpret_cast<uintptr_t>(b->first) | reinterpret_cast<uintptr_t>(b->len) | reinterpret_cast<uintptr_t>(b->page_table)) & 3u) != 0)
+    return MST_ERR_SHAPE;
+  *cache = Cache{(__nv_bfloat16*)c->K, (__nv_bfloat16*)c->V, c->page_stride, c->token_stride, c->head_stride,
+                 c->num_pages, c->page_size, c->kv_heads, c->head_dim};
+  *batch = Batch{b->first, b->len, b->page_table, b->batch, b->tokens, b->table_stride};
+  return MST_OK;
+}
+
+#ifdef __CUDACC__
+struct Slot {
+  bool exists;
+  int64_t at;    // element of the slot's first head
+};
+// Slot of position p (p >= 0) of sequence b.  `flag`: the file's own word for pages that do not exist
+__device__ __forceinline__ Slot slot_of(const Cache& C, const Batch& B, int b, int p, int* flag) {
+  int slot;
+  const int id = page_of(B.table + (int64_t)b * B.table_stride, B.table_stride, C.page_size, C.num_pages, p, slot);
+  if (id < 0) {
+    *flag = 1;
+    return Slot{false, 0};
+  }
+  return Slot{true, (int64_t)id * C.page_stride + (int64_t)slot * C.token_stride};
+}
+// The sequence that a row belongs to (a warp's question, all lanes the same row): how many sequences end at or before it.  -1: none
+__device__ __forceinline__ int sequence_of(const Batch& B, int row, int lane) {
+  int before = 0;
+  for (int i0 = 0; i0 < B.batch; i0 += 32) {
+    const bool ended = i0 + lane < B.batch && B.first[i0 + lane + 1] <= row;
+    before += __popc(__ballot_sync(0xffffffffu, ended));
+  }
+  return before < B.batch && B.first[before] <= row && row < B.first[before + 1] ? before : -1;
+}
+// The position of row `row` of sequence b, below 0 where the sequence is shorter than its new tokens
+__device__ __forceinline__ int position_of(const Batch& B, int b, int row) {
+  const int64_t p = (int64_t)B.len[b] - B.first[b + 1] + row;
+  return p < 0 ? -1 : (int)p;
+}
+// A file's word for pages that do not exist: its value, and zero from then on
+inline mst_status_t take_flag(const void* symbol, int32_t* flag) {
+  int v = 0;
+  MST_CUDA_TRY(cudaMemcpyFromSymbol(&v, symbol, sizeof(int)));
+  const int zero = 0;
+  if (v) MST_CUDA_TRY(cudaMemcpyToSymbol(symbol, &zero, sizeof(int)));
+  *flag = v;
+  return MST_OK;
+}
+#endif
+
+}  // namespace mst_paged

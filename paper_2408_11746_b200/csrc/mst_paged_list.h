@@ -1,0 +1,100 @@
+// What a tile of query rows looks at in a paged cache: index arithmetic only, the same on the host (where it is tested, also on lengths and page
+// numbers that make no sense) and on the device.
+//
+// A tile is up to R neighbours among one sequence's (new token, query head of one key head) pairs, so that the heads of a group share keys.
+// Its keys are a list: the window of all its tokens, positions w0 .. w0 + W - 1 in order; then for each m >= 1 the positions m l behind each of its
+// tokens, which only that token's rows look at.  Where a tile has l tokens or more the window is everything from 0 on and the set is left to
+// the mask.  Lists have below 2^32 entries for any lengths: the window ends at the last position and the rest has fewer than that.
+#pragma once
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define MST_HD __host__ __device__ __forceinline__
+#else
+#define MST_HD inline
+#endif
+
+namespace mst_paged {
+
+struct Key {
+  int pos;    // -1: none
+  int who;    // the token of the tile that alone looks at it, -1: the window
+};
+
+struct List {
+  int row0, rows;         // the tile's pairs among the sequence's
+  int first;              // the sequence's first row of the activations
+  int t_lo, nt;           // the tokens it touches
+  int p_lo, p_hi;         // their positions
+  int l, w0;
+  uint32_t W, N;          // entries of the window, of the list
+  bool dense;
+
+  // Tile `tile` of `R` pairs of a sequence with rows first .. end - 1 of `tokens` and `len` positions, `group` query heads to a key head, `reach`
+  // positions that its table has room for.  false: no such tile.
+  MST_HD bool locate(int first_, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R) {
+    first = first_;
+    l = stride;
+    if (first < 0 || end <= first || end > tokens) return false;
+    const int n = end - first;
+    const int64_t all = (int64_t)n * group, r0 = (int64_t)tile * R;
+    if (r0 >= all) return false;
+    row0 = (int)r0;
+    rows = all - r0 < R ? (int)(all - r0) : R;
+    t_lo = row0 / group;
+    nt = (row0 + rows - 1) / group - t_lo + 1;
+    const int64_t p = (int64_t)len - n + t_lo;
+    p_lo = p < -(1 << 30) ? -(1 << 30) : (int)p;      // a length that far below its tokens: nothing is looked at either way
+    p_hi = p_lo + nt - 1;
+    dense = nt >= l;
+    const int64_t last = p_hi < reach ? p_hi : reach - 1;
+    const int64_t w = dense ? 0 : (int64_t)p_lo - l + 1;
+    w0 = w > 0 ? (int)w : 0;
+    W = last >= w0 ? (uint32_t)(last - w0 + 1) : 0u;
+    N = W + (dense || p_hi < l ? 0u : (uint32_t)(p_hi / l) * (uint32_t)nt);
+    return true;
+  }
+  MST_HD Key key(uint32_t n) const {
+    if (n < W) return Key{w0 + (int)n, -1};
+    if (n >= N) return Key{-1, -1};
+    uint32_t m = n - W;
+    int who = 0;
+    if (nt > 1) {
+      const uint32_t f = m;
+      m = f / (uint32_t)nt;
+      who = (int)(f - m * (uint32_t)nt);
+    }
+    const int64_t p = (int64_t)p_lo + who - (int64_t)(m + 1) * l;
+    return Key{p < 0 ? -1 : (int)p, who};
+  }
+  // does the row of the tile's token `t`, at position p, look at an entry
+  MST_HD bool sees(int p, int t, Key k) const {
+    if (k.pos < 0) return false;
+    if (k.who >= 0) return k.who == t;
+    const int back = p - k.pos;       // both within 2^31 of each other: positions from -2^30 on
+    return back >= 0 && (back < l || (dense && back % l == 0));
+  }
+  // Range `split` of at most `splits` ranges of whole units of `unit` entries, `least` of them at least.  active: how many ranges there are.
+  MST_HD bool range(int splits, int least, int unit, int split, uint32_t& lo, uint32_t& hi, int& active) const {
+    const uint32_t units = N / (uint32_t)unit + (N % (uint32_t)unit != 0 ? 1u : 0u);
+    uint32_t each = units / (uint32_t)splits + (units % (uint32_t)splits != 0 ? 1u : 0u);
+    if (each < (uint32_t)least) each = (uint32_t)least;
+    active = units == 0 ? 1 : (int)(units / each + (units % each != 0 ? 1u : 0u));
+    if (split >= active) return false;
+    const uint64_t a = (uint64_t)each * (uint32_t)split * (uint32_t)unit, z = a + (uint64_t)each * (uint32_t)unit;
+    lo = (uint32_t)a;
+    hi = z < N ? (uint32_t)z : N;
+    return true;
+  }
+};
+
+// Page of position p >= 0 in a sequence's row of the table, -1 where there is none
+MST_HD int page_of(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int& slot) {
+  const int page = p / page_size;
+  slot = p - page * page_size;
+  if (page >= table_stride) return -1;
+  const int id = row[page];
+  return id >= 0 && id < num_pages ? id : -1;
+}
+
+}  // namespace mst_paged

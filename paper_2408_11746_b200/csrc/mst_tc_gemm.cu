@@ -1483,6 +1483,10 @@ extern "C" mst_status_t mst_device_error_flags(int32_t* flags) {
   int32_t f32 = 0;
   MST_TRY(mst_split_error_flags(&f32));
   v |= f32;
-  *flags = v | (att << 1) | (sp << 2) | (cc << 3);
+  int32_t paged = 0, append = 0;
+  MST_TRY(mst_paged_error_flags(&paged));
+  MST_TRY(mst_append_error_flags(&append));
+  paged |= append;
+  *flags = v | (att << 1) | (sp << 2) | (cc << 3) | (paged << 4);
   return MST_OK;
 }

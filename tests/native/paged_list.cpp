@@ -1,0 +1,48 @@
+// The index arithmetic of the paged attention for the host tests: what the rows of a tile look at, range by range.
+#include "mst_paged_list.h"
+
+using mst_paged::Key;
+using mst_paged::List;
+
+extern "C" {
+
+// info: row0, rows, t_lo, nt, p_lo, p_hi, W, N, dense; 0 where there is no such tile
+int list_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int64_t* info) {
+  List T;
+  if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return 0;
+  const int64_t v[9] = {T.row0, T.rows, T.t_lo, T.nt, T.p_lo, T.p_hi, (int64_t)T.W, (int64_t)T.N, T.dense};
+  for (int i = 0; i < 9; ++i) info[i] = v[i];
+  return 1;
+}
+
+int range_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int splits, int least, int unit,
+             int split, int64_t* lo_hi_active) {
+  List T;
+  if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return -1;
+  uint32_t lo = 0, hi = 0;
+  int active = 0;
+  const int there = T.range(splits, least, unit, split, lo, hi, active);
+  lo_hi_active[0] = lo;
+  lo_hi_active[1] = hi;
+  lo_hi_active[2] = active;
+  return there;
+}
+
+// entries lo .. hi - 1: position and token; `seen` [hi - lo][nt]: which of the tile's tokens look at them
+int keys_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int64_t lo, int64_t hi, int32_t* pos,
+            int32_t* who, uint8_t* seen) {
+  List T;
+  if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return 0;
+  for (int64_t n = lo; n < hi; ++n) {
+    const Key k = T.key((uint32_t)n);
+    pos[n - lo] = k.pos;
+    who[n - lo] = k.who;
+    for (int t = 0; t < T.nt; ++t) seen[(n - lo) * T.nt + t] = T.sees(T.p_lo + t, t, k);
+  }
+  return 1;
+}
+
+int page(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int* slot) {
+  return mst_paged::page_of(row, table_stride, page_size, num_pages, p, *slot);
+}
+}

@@ -1,0 +1,173 @@
+"""Calls of the rotation and paged-cache entry points that are refused on the host, before anything is launched (no GPU needed)."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+INVALID, SHAPE, DTYPE, CAPACITY = 1, 2, 3, 4
+A = 1 << 20          # an aligned address that nothing ever reads
+
+
+@pytest.fixture(scope="module")
+def mst():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2408_11746_b200 as m
+    return m
+
+
+def _status(mst, f, *args, **kw):
+    with pytest.raises(mst.MstError) as e:
+        f(*args, **kw)
+    return e.value.status
+
+
+def _rot(mst, D=64, rot=64, f=A, gq=A, gk=A, eps=1e-6):
+    return mst.Rotation(D, rot, f, gq, gk, eps)
+
+
+def _fwd(mst, rot=None, dtype=1, tokens=4, seq=4, positions=None, hq=2, hk=2, Q=A, K=A, ld=128, Qo=A, Ko=A, ldo=128):
+    mst.mst_qk_norm_rotate_fwd(rot if rot is not None else _rot(mst), dtype, tokens, seq, positions, hq, hk, Q, K, ld, Qo, Ko, ldo, stream=0)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), DTYPE), (dict(tokens=-1), INVALID), (dict(hq=-1), INVALID), (dict(seq=0), INVALID), (dict(Q=None), INVALID),
+    (dict(Ko=None), INVALID), (dict(ld=120), SHAPE), (dict(ldo=100), SHAPE), (dict(ld=132), SHAPE), (dict(Q=A + 8), SHAPE),
+    (dict(Ko=A + 2), SHAPE), (dict(tokens=1 << 32), SHAPE), (dict(positions=A + 1), SHAPE), (dict(hq=65536, ld=1 << 23, ldo=1 << 23), SHAPE)])
+def test_forward(mst, kw, status):
+    assert _status(mst, _fwd, mst, **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(D=60), SHAPE), (dict(D=264), SHAPE), (dict(D=0), SHAPE), (dict(rot=8), SHAPE), (dict(rot=80), SHAPE), (dict(rot=-16), SHAPE),
+    (dict(f=None), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(gq=A + 4), SHAPE), (dict(f=A + 2), SHAPE)])
+def test_rotation(mst, kw, status):
+    assert _status(mst, _fwd, mst, rot=_rot(mst, **kw)) == status
+    assert _status(mst, mst.mst_qk_norm_rotate_bwd_workspace, _rot(mst, **kw), 4) == status
+
+
+def test_forward_of_nothing(mst):
+    _fwd(mst, tokens=0)
+    _fwd(mst, hq=0, hk=0, Q=None, K=None, Qo=None, Ko=None)
+
+
+def _bwd(mst, rot=None, dtype=1, tokens=4, hq=2, hk=2, Q=A, K=A, ld=128, dQo=A, dKo=A, lddo=128, dQ=A, dK=A, ldg=128, gq=A, gk=A, ws=A,
+         ws_bytes=1 << 20):
+    rot = rot if rot is not None else _rot(mst)
+    mst._check(mst._lib.mst_qk_norm_rotate_bwd(rot, dtype, tokens, 4, None, hq, hk, Q, K, ld, dQo, dKo, lddo, dQ, dK, ldg, gq, gk, ws, ws_bytes,
+                                               None), "mst_qk_norm_rotate_bwd")
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=9), DTYPE), (dict(Q=None), INVALID), (dict(dKo=None), INVALID), (dict(dQ=None), INVALID), (dict(ldg=64), SHAPE),
+    (dict(lddo=129), SHAPE), (dict(dQ=A + 4), SHAPE), (dict(gq=A + 2), SHAPE), (dict(ws=A + 4), SHAPE), (dict(ws=None), CAPACITY),
+    (dict(ws_bytes=100), CAPACITY)])
+def test_gradients(mst, kw, status):
+    assert _status(mst, _bwd, mst, **kw) == status
+
+
+def test_weight_gradient_without_a_weight(mst):
+    assert _status(mst, _bwd, mst, rot=_rot(mst, gk=None)) == INVALID
+    assert mst.mst_qk_norm_rotate_bwd_workspace(_rot(mst, gq=None, gk=None), 100) == 0
+    assert mst.mst_qk_norm_rotate_bwd_workspace(_rot(mst), 100) > 0
+
+
+def _cache(mst, **kw):
+    c = mst.PagedCache(torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16), torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16))
+    c.K = c.V = A
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def _batch(mst, **kw):
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    b = mst.PagedBatch(i(3), i(2), i(2, 4), 8, 4, 64)
+    b.first = b.len = b.page_table = A
+    for k, v in kw.items():
+        setattr(b, k, v)
+    return b
+
+
+BAD_CACHE = [(dict(K=None), INVALID), (dict(V=None), INVALID), (dict(page_size=0), INVALID), (dict(num_pages=-1), INVALID),
+             (dict(kv_heads=0), INVALID), (dict(token_stride=100), SHAPE), (dict(token_stride=56), SHAPE), (dict(head_stride=8), SHAPE),
+             (dict(page_stride=-2048), SHAPE), (dict(page_stride=8), SHAPE), (dict(K=A + 8), SHAPE)]
+BAD_BATCH = [(dict(batch=-1), INVALID), (dict(tokens=-1), INVALID), (dict(first=None), INVALID), (dict(len=None), INVALID),
+             (dict(page_table=None), INVALID), (dict(max_new=-1), INVALID), (dict(table_stride=-1), INVALID), (dict(first=A + 2), SHAPE),
+             (dict(page_table=A + 1), SHAPE), (dict(batch=65536), SHAPE)]
+
+
+def _append(mst, cache=None, batch=None, rot=None, heads=2, Q=A, K=A, V=A, ld=128, Qo=A, ldq=128):
+    mst.mst_paged_append(cache or _cache(mst), batch or _batch(mst), rot, heads, Q, K, V, ld, Qo, ldq, stream=0)
+
+
+def _attend(mst, cache=None, batch=None, heads=2, stride=64, Q=A, ldq=128, Out=A, ldo=128, lse=A, ws=A, ws_bytes=1 << 30):
+    mst._check(mst._lib.mst_paged_attention(cache or _cache(mst), batch or _batch(mst), heads, stride, Q, ldq, Out, ldo, lse, ws, ws_bytes, None),
+               "mst_paged_attention")
+
+
+@pytest.mark.parametrize("kw,status", BAD_CACHE)
+def test_caches(mst, kw, status):
+    assert _status(mst, _append, mst, cache=_cache(mst, **kw)) == status
+    assert _status(mst, _attend, mst, cache=_cache(mst, **kw)) == status
+    assert _status(mst, mst.mst_paged_attention_workspace, _cache(mst, **kw), _batch(mst), 2, 64) == status
+
+
+@pytest.mark.parametrize("kw,status", BAD_BATCH)
+def test_batches(mst, kw, status):
+    assert _status(mst, _append, mst, batch=_batch(mst, **kw)) == status
+    assert _status(mst, _attend, mst, batch=_batch(mst, **kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(K=None), INVALID), (dict(V=None), INVALID), (dict(heads=-1), INVALID), (dict(Q=None), INVALID), (dict(Qo=None), INVALID),
+    (dict(ld=64), SHAPE), (dict(ldq=100), SHAPE), (dict(V=A + 8), SHAPE), (dict(Qo=A + 4), SHAPE), (dict(heads=65536), SHAPE)])
+def test_append(mst, kw, status):
+    assert _status(mst, _append, mst, **kw) == status
+
+
+def test_append_with_a_rotation_of_another_width(mst):
+    assert _status(mst, _append, mst, rot=_rot(mst, D=128)) == SHAPE
+    assert _status(mst, _append, mst, cache=_cache(mst, head_dim=60)) == SHAPE
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(heads=0), INVALID), (dict(heads=3), SHAPE), (dict(stride=0), INVALID), (dict(Q=None), INVALID), (dict(Out=None), INVALID),
+    (dict(ldq=64), SHAPE), (dict(ldo=132), SHAPE), (dict(Q=A + 2), SHAPE), (dict(lse=A + 2), SHAPE), (dict(ws=A + 8), SHAPE)])
+def test_attention(mst, kw, status):
+    assert _status(mst, _attend, mst, **kw) == status
+
+
+def test_attention_head_dims_and_workspaces(mst):
+    for d in (32, 72, 256):
+        assert _status(mst, _attend, mst, cache=_cache(mst, head_dim=d, token_stride=512, head_stride=256, page_stride=8192), ldq=512,
+                       ldo=512) == SHAPE
+    long = _batch(mst, max_len=8192, table_stride=512)
+    need = mst.mst_paged_attention_workspace(_cache(mst), long, 2, 1 << 30)
+    assert need > 0
+    assert _status(mst, _attend, mst, batch=long, stride=1 << 30, ws=None, ws_bytes=0) == CAPACITY
+    assert _status(mst, _attend, mst, batch=long, stride=1 << 30, ws_bytes=need - 1) == CAPACITY
+    # distance one divides every distance: the same as no stride at all
+    assert mst.mst_paged_attention_workspace(_cache(mst), long, 2, 1) == need
+
+
+def test_calls_without_sequences(mst):
+    none = _batch(mst, batch=0, first=None, len=None, page_table=None)
+    _append(mst, batch=none)
+    _attend(mst, batch=none)
+    _attend(mst, batch=_batch(mst, tokens=0))
+
+
+def test_structures_check_their_tensors(mst):
+    z = torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16)
+    for K, V in ((z, z[:2]), (z.float(), z.float()), (z, z.transpose(1, 2).contiguous().transpose(1, 2)), (z[..., ::2], z[..., ::2]), (z[0], z[0])):
+        with pytest.raises(ValueError):
+            mst.PagedCache(K, V)
+    t = z.transpose(1, 2).contiguous().transpose(1, 2)
+    assert (mst.PagedCache(t, t).token_stride, mst.PagedCache(t, t).head_stride) == (64, 1024)
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for a in ((i(2), i(2), i(2, 4)), (i(3), i(2), i(3, 4)), (i(3).long(), i(2), i(2, 4)), (i(3), i(2), i(2, 8)[:, ::2]), (i(3), i(2), i(2))):
+        with pytest.raises(ValueError):
+            mst.PagedBatch(*a, 4, 1, 1)
+    assert ctypes.sizeof(mst.PagedCache) == 56 and ctypes.sizeof(mst.PagedBatch) == 48 and ctypes.sizeof(mst.Rotation) == 40

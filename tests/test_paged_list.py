@@ -1,0 +1,119 @@
+"""The paged attention's index arithmetic on the host: every row looks at exactly its set, once, over all ranges of its tile's list, and lengths
+or page numbers that make no sense name no memory."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("native") / "paged_list.so")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover=undefined",
+                    "-static-libubsan", "-I", os.path.join(ROOT, "paper_2408_11746_b200", "csrc"),
+                    os.path.join(ROOT, "tests", "native", "paged_list.cpp"), "-o", so], check=True)
+    return ctypes.CDLL(so)
+
+
+def _args(first, n, length, group, stride, reach, tile, R):
+    return [first, first + n, length, first + n + 3, group, stride, ctypes.c_int64(reach), tile, R]
+
+
+def _tile(lib, args):
+    info = (ctypes.c_int64 * 9)()
+    return list(info) if lib.list_of(*args, info) else None
+
+
+def _seen_by_rows(lib, n, length, group, stride, R, splits, least, unit, reach=BIG):
+    """{row of the sequence: positions it looks at, in list order over all ranges}"""
+    out, tile = {}, 0
+    while True:
+        args = _args(5, n, length, group, stride, reach, tile, R)
+        info = _tile(lib, args)
+        if info is None:
+            return out
+        row0, rows, t_lo, nt, p_lo, p_hi, W, N, dense = info
+        assert p_lo == length - n + t_lo and p_hi == p_lo + nt - 1 and rows <= R and row0 == tile * R
+        seen = {t: [] for t in range(nt)}
+        end, split = 0, 0
+        while True:
+            lha = (ctypes.c_int64 * 3)()
+            there = lib.range_of(*args, splits, least, unit, split, lha)
+            if not there:
+                break
+            lo, hi, active = list(lha)
+            assert lo == end and hi >= lo and (hi > lo or N == 0) and split < active <= splits
+            assert lo % unit == 0
+            end = hi
+            pos, who = np.empty(hi - lo, np.int32), np.empty(hi - lo, np.int32)
+            got = np.empty((hi - lo, nt), np.uint8)
+            lib.keys_of(*args, ctypes.c_int64(lo), ctypes.c_int64(hi), pos.ctypes, who.ctypes, got.ctypes)
+            for t in range(nt):
+                seen[t] += pos[got[:, t] != 0].tolist()
+            split += 1
+        assert end == N and split == active
+        for r in range(row0, row0 + rows):
+            out[r] = seen[r // group - t_lo]
+        tile += 1
+
+
+@pytest.mark.parametrize("stride", [1 << 30, 64, 128, 100, 7, 3, 2])
+@pytest.mark.parametrize("n,length,group,R", [(1, 1, 1, 16), (1, 700, 1, 16), (1, 129, 5, 16), (5, 300, 2, 16), (7, 7, 3, 16), (40, 333, 1, 32),
+                                              (9, 200, 40, 32), (130, 400, 1, 128), (70, 500, 4, 128), (3, 2, 2, 16), (4, 0, 1, 16)])
+def test_rows_look_at_their_sets(lib, n, length, group, R, stride):
+    got = _seen_by_rows(lib, n, length, group, stride, R, splits=3, least=2, unit=16)
+    assert sorted(got) == list(range(n * group))
+    for r, seen in got.items():
+        i = length - n + r // group
+        want = [j for j in range(i + 1) if i - j < stride or (i - j) % stride == 0]
+        assert sorted(seen) == want and len(set(seen)) == len(seen)
+
+
+def test_rows_stay_within_the_table(lib):
+    got = _seen_by_rows(lib, 4, 100, 1, 64, 16, 2, 1, 16, reach=80)
+    for r, seen in got.items():
+        i = 96 + r
+        assert set(seen) >= {j for j in range(80) if 0 <= i - j < 64}
+
+
+@pytest.mark.parametrize("first,end,tokens", [(0, 0, 10), (5, 4, 10), (-1, 3, 10), (4, 11, 10), (-(1 << 31), (1 << 31) - 1, 10)])
+def test_rows_that_are_not_there(lib, first, end, tokens):
+    info = (ctypes.c_int64 * 9)()
+    assert not lib.list_of(first, end, 100, tokens, 1, 64, ctypes.c_int64(BIG), 0, 16, info)
+
+
+@pytest.mark.parametrize("length", [-(1 << 31), -5, 0, (1 << 31) - 1, (1 << 30) + 7])
+@pytest.mark.parametrize("stride", [2, 64, (1 << 31) - 1])
+@pytest.mark.parametrize("reach", [0, 4096, BIG])
+def test_lengths_that_make_no_sense(lib, length, stride, reach):
+    args = _args(0, 33, length, 1, stride, reach, 1, 16)
+    row0, rows, t_lo, nt, p_lo, p_hi, W, N, dense = _tile(lib, args)
+    assert 0 <= W <= N < 1 << 32 and W <= max(0, reach)
+    if length <= 0:
+        assert N == 0
+    lha = (ctypes.c_int64 * 3)()
+    assert lib.range_of(*args, 64, 4, 64, 0, lha) == 1
+    for n in {0, W // 2, max(W - 1, 0), W, min(W + 1, max(N - 1, 0)), max(N - 1, 0), N}:
+        pos, who, got = np.empty(1, np.int32), np.empty(1, np.int32), np.empty((1, nt), np.uint8)
+        lib.keys_of(*args, ctypes.c_int64(n), ctypes.c_int64(n + 1), pos.ctypes, who.ctypes, got.ctypes)
+        assert -1 <= pos[0] <= max(p_hi, 0) and -1 <= who[0] < nt
+        if n >= N:
+            assert pos[0] == -1 and not got.any()
+
+
+def test_pages_that_do_not_exist(lib):
+    row = np.array([3, -1, 9, 8, -(1 << 31), (1 << 31) - 1], np.int32)
+    slot = ctypes.c_int()
+    want = {0: 3, 1: -1, 2: -1, 3: 8, 4: -1, 5: -1, 6: -1, 100: -1}
+    for page, id_ in want.items():
+        for p in (page * 7, page * 7 + 6):
+            assert lib.page(row.ctypes, len(row), 7, 9, p, ctypes.byref(slot)) == id_
+            assert slot.value == p % 7
+    assert lib.page(row.ctypes, 0, 7, 9, 0, ctypes.byref(slot)) == -1
+    assert lib.page(row.ctypes, len(row), 1, 9, (1 << 31) - 1, ctypes.byref(slot)) == -1
+    assert lib.page(row.ctypes, len(row), 1, 0, 0, ctypes.byref(slot)) == -1
