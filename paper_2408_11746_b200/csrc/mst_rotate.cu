@@ -19,59 +19,66 @@ struct RowsParams {
   int hq, hk;
   const int32_t* positions;
   int seq_len;
-  int64_t tokens;
-  int share, per_warp;         // warps of a token, steps of a warp
+  int tokens;
+  int per_warp;                // steps of a warp
   mst_paged::Cache cache;
   mst_paged::Batch batch;
 };
 
 constexpr int AHEAD = 4;       // steps whose loads are in flight together
 
-template <typename T, int G, bool APPEND>
-__global__ void __launch_bounds__(32 * WARPS) rotate_rows_kernel(const RowsParams P) {
-  __shared__ float2 tables[WARPS][MAX_HALF];
+template <typename T, int G, bool INTER, bool APPEND>
+__global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid_constant__ RowsParams P) {
+  __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
   constexpr int ROWS = 32 / G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
-  const int64_t w = (int64_t)blockIdx.x * WARPS + warp;
-  const int64_t token = w / P.share;
-  if (token >= P.tokens) return;
+  const unsigned at = blockIdx.x * WARPS + warp;
+  if (at >= (unsigned)P.tokens) return;
+  const int token = (int)at;
   const Steps steps(ROWS, P.hq, P.hk, APPEND ? P.hk : 0);
-  const int begin = (int)(w - token * P.share) * P.per_warp;
+  const int begin = (int)blockIdx.y * P.per_warp;
   const int end = begin + P.per_warp < steps.all() ? begin + P.per_warp : steps.all();
-  const Lane L(P.R, lane % G, lane);
+  const Lane L(P.R, lane % G, INTER);
   const int row = lane / G;
+  const int64_t jump = (int64_t)row * P.R.D;                                    // this lane's row of a step
+  const T* in_q = (const T*)P.Q + token * P.ld + jump;
+  const T* in_k = (const T*)P.K + token * P.ld + jump;
+  const T* in_v = APPEND ? (const T*)P.V + token * P.ld + jump : nullptr;
+  // side of a step, its rows' first head
   auto side_of = [&](int i, int& head) {
-    const int side = i < steps.q ? 0 : i < steps.q + steps.k ? 1 : 2;
-    head = (i - (side == 0 ? 0 : side == 1 ? steps.q : steps.q + steps.k)) * ROWS + row;
+    const int side = i < steps.q ? 0 : !APPEND || i < steps.q + steps.k ? 1 : 2;
+    head = (side == 0 ? i : side == 1 ? i - steps.q : i - steps.q - steps.k) * ROWS;
     return side;
   };
-  auto fetch = [&](int i) {
+  auto fetch = [&](int i, Raw<T>& r) {
     int head;
     const int side = side_of(i, head);
-    const T* base = (const T*)(side == 0 ? P.Q : side == 1 ? P.K : P.V);
-    const bool in = i < end && head < (side == 0 ? P.hq : P.hk) && L.e0 < P.R.D;
-    return in ? load8<T>(base + token * P.ld + (int64_t)head * P.R.D + L.e0) : zero8<T>();
+    no_row(r);
+    if (i < end && L.in && head + row < (side == 0 ? P.hq : P.hk)) load_row(r, (side == 0 ? in_q : side == 1 ? in_k : in_v) + head * P.R.D, L);
   };
   Raw<T> raw[AHEAD];
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) raw[u] = fetch(begin + u);
+  for (int u = 0; u < AHEAD; ++u) fetch(begin + u, raw[u]);
   int pos;
   mst_paged::Slot slot = {true, 0};
   if (APPEND) {
-    const int b = mst_paged::sequence_of(P.batch, (int)token, lane);
+    const int b = mst_paged::sequence_of(P.batch, token, lane);
     if (b < 0) return;
-    pos = mst_paged::position_of(P.batch, b, (int)token);
+    pos = mst_paged::position_of(P.batch, b, token);
     if (pos < 0) return;
     slot = mst_paged::slot_of(P.cache, P.batch, b, pos, &g_bad_page);
   } else {
-    pos = P.positions ? P.positions[token] : (int)(token % P.seq_len);
+    pos = P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len);
   }
-  angles(tables[warp], P.R, pos, lane);
-  const Turn turn = turn_of(P.R, L, tables[warp], false);
-  float A[8], B[8];
-  const float* gamma = nullptr;
+  T* out_q = (T*)P.Qo + token * P.ldq + jump;
+  T* out_k = APPEND ? (T*)P.cache.K + slot.at + row * P.cache.head_stride : (T*)P.Ko + token * P.ldq + jump;
+  T* out_v = APPEND ? (T*)P.cache.V + slot.at + row * P.cache.head_stride : nullptr;
+  const Turn turn = turn_of<INTER>(tables[warp], P.R, L, pos, lane);
+  const float inv_d = 1.f / (float)P.R.D;
+  Pairs A = {}, B = {};      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
+  bool norm = false;
   int cur = -1;
   for (int i0 = begin; i0 < end; i0 += AHEAD) {
 #pragma unroll
@@ -80,43 +87,55 @@ __global__ void __launch_bounds__(32 * WARPS) rotate_rows_kernel(const RowsParam
       if (i >= end) break;
       int head;
       const int side = side_of(i, head);
-      if (side != cur && side < 2) {
-        gamma = side == 0 ? P.R.gamma_q : P.R.gamma_k;
-        weights(P.R, L, gamma, A, B);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          A[e] *= turn.c[e];
-          B[e] *= turn.s[e];
-        }
-        cur = side;
-      }
       Raw<T> out = raw[u];
       if (!APPEND || side < 2) {
-        float x[8], p[8];
-        widen(raw[u], x);
-        partners(P.R, L, raw[u], x, p);
-        float r = 1.f;
-        if (gamma) {
-          float sq = 0.f;
+        if (side != cur) {
+          const float* gamma = side == 0 ? P.R.gamma_q : P.R.gamma_k;
+          norm = gamma != nullptr;
+          const Pairs g = weights<INTER>(gamma, L);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sq = fmaf(x[e], x[e], sq);
-          r = rsqrtf(sum_lanes<G>(sq) / (float)P.R.D + P.R.eps);
+          for (int k = 0; k < 2; ++k) {
+            A.u[k] = mul2(g.u[k], turn.c[k]);
+            A.v[k] = mul2(g.u[k], turn.s[k]);
+            B.u[k] = negated(mul2(g.v[k], turn.s[k]));
+            B.v[k] = mul2(g.v[k], turn.c[k]);
+          }
+          cur = side;
         }
+        const Pairs x = widen<INTER>(raw[u]);
+        Pairs y;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = r * fmaf(p[e], B[e], x[e] * A[e]);
-        narrow(x, out);
+        for (int k = 0; k < 2; ++k) {
+          y.u[k] = fma2(x.v[k], B.u[k], mul2(x.u[k], A.u[k]));
+          y.v[k] = fma2(x.v[k], B.v[k], mul2(x.u[k], A.v[k]));
+        }
+        if (P.R.rot < P.R.D && !L.turns) {     // no pairs: an infinite value stays on its own
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            y.u[k] = mul2(x.u[k], A.u[k]);
+            y.v[k] = mul2(x.v[k], B.v[k]);
+          }
+        }
+        if (norm) {
+          const float r = rsqrtf(fmaf(sum_lanes<G>(dot(x, x)), inv_d, P.R.eps));
+          const uint64_t r2 = pack2(r, r);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            y.u[k] = mul2(y.u[k], r2);
+            y.v[k] = mul2(y.v[k], r2);
+          }
+        }
+        narrow<INTER>(y, out);
       }
-      if (head < (side == 0 ? P.hq : P.hk) && L.e0 < P.R.D) {
-        if (side == 0 || !APPEND) {
-          store8<T>((T*)(side == 0 ? P.Qo : P.Ko) + token * P.ldq + (int64_t)head * P.R.D + L.e0, out);
-        } else if (slot.exists) {
-          store8<T>((T*)(side == 1 ? P.cache.K : P.cache.V) + slot.at + (int64_t)head * P.cache.head_stride + L.e0, out);
-        }
+      if (L.in && head + row < (side == 0 ? P.hq : P.hk)) {
+        if (side == 0) store_row(out, out_q + head * P.R.D, L);
+        else if (!APPEND) store_row(out, out_k + head * P.R.D, L);
+        else if (slot.exists) store_row(out, (side == 1 ? out_k : out_v) + head * P.cache.head_stride, L);
       }
     }
     if (i0 + AHEAD < end) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) raw[u] = fetch(i0 + AHEAD + u);
+      for (int u = 0; u < AHEAD; ++u) fetch(i0 + AHEAD + u, raw[u]);
     }
   }
 }
@@ -130,7 +149,7 @@ struct GradParams {
   int hq, hk;
   const int32_t* positions;
   int seq_len;
-  int64_t tokens;
+  int tokens;
   int share, per_warp;
   float* partial;        // [blocks][2][D]: sums of the weights' gradients, or NULL
 };
@@ -140,113 +159,116 @@ struct GradParams {
 constexpr int GRAD_BLOCKS_PER_SM = 2, GRAD_AHEAD = 2;
 constexpr int GRAD_BLOCKS_MOST = 512;
 
-template <typename T, int G>
-__global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_kernel(const GradParams P) {
-  __shared__ float2 tables[WARPS][MAX_HALF];
+template <typename T, int G, bool INTER>
+__global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_kernel(const __grid_constant__ GradParams P) {
+  __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
   constexpr int ROWS = 32 / G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
   const Steps steps(ROWS, P.hq, P.hk, 0);
-  const Lane L(P.R, lane % G, lane);
+  const Lane L(P.R, lane % G, INTER);
   const int row = lane / G;
-  const bool in_row = L.e0 < P.R.D;
-  float acc[2][8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[0][e] = acc[1][e] = 0.f;
-  const int64_t all = P.tokens * P.share;
-  for (int64_t w = (int64_t)blockIdx.x * WARPS + warp; w < all; w += (int64_t)gridDim.x * WARPS) {
-    const int64_t token = w / P.share;
-    const int begin = (int)(w - token * P.share) * P.per_warp;
+  const int64_t jump = (int64_t)row * P.R.D;
+  const float inv_d = 1.f / (float)P.R.D;
+  const Pairs gq = weights<INTER>(P.R.gamma_q, L), gk = weights<INTER>(P.R.gamma_k, L);
+  Pairs acc_q = {}, acc_k = {};
+  const unsigned groups = ((unsigned)P.tokens + WARPS - 1) / WARPS, all = groups * (unsigned)P.share;
+  for (unsigned unit = blockIdx.x; unit < all; unit += gridDim.x) {
+    const unsigned part = P.share > 1 ? unit / groups : 0u, at = (unit - part * groups) * WARPS + warp;
+    if (at >= (unsigned)P.tokens) continue;
+    const int token = (int)at;
+    const int begin = (int)part * P.per_warp;
     const int end = begin + P.per_warp < steps.all() ? begin + P.per_warp : steps.all();
+    const T *x_q = (const T*)P.Q + token * P.ld + jump, *x_k = (const T*)P.K + token * P.ld + jump;
+    const T *y_q = (const T*)P.dQo + token * P.lddo + jump, *y_k = (const T*)P.dKo + token * P.lddo + jump;
+    T *d_q = (T*)P.dQ + token * P.ldg + jump, *d_k = (T*)P.dK + token * P.ldg + jump;
     Raw<T> rx[GRAD_AHEAD], ry[GRAD_AHEAD];
     auto fetch = [&](int i, Raw<T>& x, Raw<T>& y) {
       const bool q = i < steps.q;
-      const int head = (q ? i : i - steps.q) * ROWS + row;
-      const bool in = i < end && head < (q ? P.hq : P.hk) && in_row;
-      const int64_t at = (int64_t)head * P.R.D + L.e0;
-      x = in && (q ? P.R.gamma_q : P.R.gamma_k) ? load8<T>((const T*)(q ? P.Q : P.K) + token * P.ld + at) : zero8<T>();
-      y = in ? load8<T>((const T*)(q ? P.dQo : P.dKo) + token * P.lddo + at) : zero8<T>();
+      const int head = (q ? i : i - steps.q) * ROWS;
+      no_row(x);
+      no_row(y);
+      if (i < end && L.in && head + row < (q ? P.hq : P.hk)) {
+        load_row(y, (q ? y_q : y_k) + head * P.R.D, L);
+        if (q ? P.R.gamma_q : P.R.gamma_k) load_row(x, (q ? x_q : x_k) + head * P.R.D, L);
+      }
     };
 #pragma unroll
     for (int u = 0; u < GRAD_AHEAD; ++u) fetch(begin + u, rx[u], ry[u]);
-    angles(tables[warp], P.R, P.positions ? P.positions[token] : (int)(token % P.seq_len), lane);
-    const Turn turn = turn_of(P.R, L, tables[warp], true);
+    const Turn turn = turn_of<INTER>(tables[warp], P.R, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
     for (int i0 = begin; i0 < end; i0 += GRAD_AHEAD) {
-      Raw<T> nx[GRAD_AHEAD], ny[GRAD_AHEAD];
-      if (i0 + GRAD_AHEAD < end) {
-#pragma unroll
-        for (int u = 0; u < GRAD_AHEAD; ++u) fetch(i0 + GRAD_AHEAD + u, nx[u], ny[u]);
-      }
 #pragma unroll
       for (int u = 0; u < GRAD_AHEAD; ++u) {
         const int i = i0 + u;
         if (i >= end) break;
         const bool q = i < steps.q;
-        const int head = (q ? i : i - steps.q) * ROWS + row;
-        const float* gamma = q ? P.R.gamma_q : P.R.gamma_k;
-        float y[8], z[8], p[8];
-        widen(ry[u], y);
-        partners(P.R, L, ry[u], y, p);
+        const int head = (q ? i : i - steps.q) * ROWS;
+        const Pairs y = widen<INTER>(ry[u]), x = widen<INTER>(rx[u]);
+        if (i + GRAD_AHEAD < end) fetch(i + GRAD_AHEAD, rx[u], ry[u]);
+        Pairs z;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = fmaf(p[e], turn.s[e], y[e] * turn.c[e]);
-        if (gamma) {
-          float x[8], g[8], sq = 0.f, dot = 0.f;
-          widen(rx[u], x);
+        for (int k = 0; k < 2; ++k) {
+          z.u[k] = fma2(y.v[k], turn.s[k], mul2(y.u[k], turn.c[k]));
+          z.v[k] = fma2(y.u[k], negated(turn.s[k]), mul2(y.v[k], turn.c[k]));
+        }
+        if (P.R.rot < P.R.D && !L.turns) z = y;
+        if (q ? P.R.gamma_q : P.R.gamma_k) {
+          Pairs g;        // z gamma
+          float r, back;
+          if (q) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) g[e] = 0.f;
-          if (in_row) {
-            const float4 a = *reinterpret_cast<const float4*>(gamma + L.e0), b = *reinterpret_cast<const float4*>(gamma + L.e0 + 4);
-            g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w; g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
+            for (int k = 0; k < 2; ++k) { g.u[k] = mul2(z.u[k], gq.u[k]); g.v[k] = mul2(z.v[k], gq.v[k]); }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) { g.u[k] = mul2(z.u[k], gk.u[k]); g.v[k] = mul2(z.v[k], gk.v[k]); }
           }
+          r = rsqrtf(fmaf(sum_lanes<G>(dot(x, x)), inv_d, P.R.eps));
+          back = -r * r * (sum_lanes<G>(dot(g, x)) * inv_d);
+          const uint64_t r2 = pack2(r, r), b2 = pack2(back, back);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            sq = fmaf(x[e], x[e], sq);
-            dot = fmaf(z[e] * g[e], x[e], dot);
-          }
-          const float inv = 1.f / (float)P.R.D;
-          const float r = rsqrtf(sum_lanes<G>(sq) * inv + P.R.eps);
-          const float back = r * r * (sum_lanes<G>(dot) * inv);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float add = z[e] * x[e] * r;
-            if (q) acc[0][e] += add; else acc[1][e] += add;
-            z[e] = r * fmaf(-back, x[e], z[e] * g[e]);
+          for (int k = 0; k < 2; ++k) {
+            const uint64_t nu = mul2(x.u[k], r2), nv = mul2(x.v[k], r2);
+            if (q) {
+              acc_q.u[k] = fma2(z.u[k], nu, acc_q.u[k]);
+              acc_q.v[k] = fma2(z.v[k], nv, acc_q.v[k]);
+            } else {
+              acc_k.u[k] = fma2(z.u[k], nu, acc_k.u[k]);
+              acc_k.v[k] = fma2(z.v[k], nv, acc_k.v[k]);
+            }
+            z.u[k] = mul2(r2, fma2(b2, x.u[k], g.u[k]));
+            z.v[k] = mul2(r2, fma2(b2, x.v[k], g.v[k]));
           }
         }
-        if (head < (q ? P.hq : P.hk) && in_row) {
+        if (L.in && head + row < (q ? P.hq : P.hk)) {
           Raw<T> out;
-          narrow(z, out);
-          store8<T>((T*)(q ? P.dQ : P.dK) + token * P.ldg + (int64_t)head * P.R.D + L.e0, out);
+          narrow<INTER>(z, out);
+          store_row(out, (q ? d_q : d_k) + head * P.R.D, L);
         }
-      }
-#pragma unroll
-      for (int u = 0; u < GRAD_AHEAD; ++u) {
-        rx[u] = nx[u];
-        ry[u] = ny[u];
       }
     }
   }
   if (!P.partial) return;
   // rows of a warp, then the warps, in a fixed order; the tables' place is free once every warp is here
-  float* sums = reinterpret_cast<float*>(tables);   // [WARPS][G * 8]: 8 * 256 floats at most
+  float* sums = reinterpret_cast<float*>(tables);   // [WARPS][D]: 8 * 256 floats at most
   static_assert(sizeof(tables) >= sizeof(float) * WARPS * 256, "a block's sums fit the tables");
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     __syncthreads();
+    float v[8];
+    values_of<INTER>(side == 0 ? acc_q : acc_k, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float v = acc[side][e];
 #pragma unroll
-      for (int o = G; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane < G) sums[warp * (G * 8) + lane * 8 + e] = v;
+      for (int o = G; o < 32; o *= 2) v[e] += __shfl_xor_sync(0xffffffffu, v[e], o);
+      if (lane < G && L.in) sums[warp * P.R.D + (e < 4 ? L.near + e : L.far + e - 4)] = v[e];
     }
     __syncthreads();
     for (int e = threadIdx.x; e < P.R.D; e += 32 * WARPS) {
-      float v = 0.f;
+      float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < WARPS; ++k) v += sums[k * (G * 8) + e];
-      P.partial[((int64_t)blockIdx.x * 2 + side) * P.R.D + e] = v;
+      for (int k = 0; k < WARPS; ++k) t += sums[k * P.R.D + e];
+      P.partial[((int64_t)blockIdx.x * 2 + side) * P.R.D + e] = t;
     }
   }
 }
@@ -276,54 +298,54 @@ __global__ void __launch_bounds__(1024) rotate_weight_grad_kernel(const float* p
 // ------------------------------------------------------------------------------------------------------------ the calls
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
-template <typename T, int G, bool APPEND>
+template <typename T, int G, bool INTER, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
   const Steps steps(32 / G, P.hq, P.hk, APPEND ? P.hk : 0);
-  P.share = warps_of_token(P.tokens, steps.all());
-  P.per_warp = (steps.all() + P.share - 1) / P.share;
-  P.share = (steps.all() + P.per_warp - 1) / P.per_warp;
-  const int64_t blocks = (P.tokens * P.share + WARPS - 1) / WARPS;
-  if (blocks > 0x7FFFFFFF) return MST_ERR_SHAPE;
-  MST_CUDA_TRY(mst_launch_overlapped(rotate_rows_kernel<T, G, APPEND>, dim3((unsigned)blocks), dim3(32 * WARPS), 0, s, P));
+  const int share = share_token(P.tokens, steps.all(), &P.per_warp);
+  const unsigned blocks = ((unsigned)P.tokens + WARPS - 1) / WARPS;
+  if (share > 65535) return MST_ERR_SHAPE;
+  MST_CUDA_TRY(mst_launch_overlapped(rotate_rows_kernel<T, G, INTER, APPEND>, dim3(blocks, (unsigned)share), dim3(32 * WARPS), 0, s, P));
   return MST_OK;
+}
+template <typename T, bool INTER, bool APPEND>
+mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
+  switch (lanes_of(P.R.D)) {
+    case 4: return launch_rows<T, 4, INTER, APPEND>(P, s);
+    case 8: return launch_rows<T, 8, INTER, APPEND>(P, s);
+    case 16: return launch_rows<T, 16, INTER, APPEND>(P, s);
+    default: return launch_rows<T, 32, INTER, APPEND>(P, s);
+  }
 }
 template <typename T, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
-  switch (lanes_of(P.R.D)) {
-    case 1: return launch_rows<T, 1, APPEND>(P, s);
-    case 2: return launch_rows<T, 2, APPEND>(P, s);
-    case 4: return launch_rows<T, 4, APPEND>(P, s);
-    case 8: return launch_rows<T, 8, APPEND>(P, s);
-    case 16: return launch_rows<T, 16, APPEND>(P, s);
-    default: return launch_rows<T, 32, APPEND>(P, s);
-  }
+  return P.R.inter ? launch_rows<T, true, APPEND>(P, s) : launch_rows<T, false, APPEND>(P, s);
 }
-template <typename T, int G>
+template <typename T, int G, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
   const Steps steps(32 / G, P.hq, P.hk, 0);
-  P.share = warps_of_token(P.tokens, steps.all());
-  P.per_warp = (steps.all() + P.share - 1) / P.share;
-  P.share = (steps.all() + P.per_warp - 1) / P.per_warp;
-  int64_t blocks = (P.tokens * P.share + WARPS - 1) / WARPS;
+  P.share = share_token(P.tokens, steps.all(), &P.per_warp);
+  int64_t blocks = ((int64_t)P.tokens + WARPS - 1) / WARPS * P.share;
   const int64_t most = (int64_t)GRAD_BLOCKS_PER_SM * mst_sm_count();
   if (blocks > most) blocks = most;
   if (blocks > GRAD_BLOCKS_MOST) blocks = GRAD_BLOCKS_MOST;
-  MST_CUDA_TRY(mst_launch_overlapped(rotate_grad_kernel<T, G>, dim3((unsigned)blocks), dim3(32 * WARPS), 0, s, P));
+  MST_CUDA_TRY(mst_launch_overlapped(rotate_grad_kernel<T, G, INTER>, dim3((unsigned)blocks), dim3(32 * WARPS), 0, s, P));
   if (P.partial)
     MST_CUDA_TRY(mst_launch_overlapped(rotate_weight_grad_kernel, dim3((unsigned)((2 * P.R.D + 31) / 32)), dim3(1024), 0, s,
                                        (const float*)P.partial, (int)blocks, P.R.D, dgamma_q, dgamma_k));
   return MST_OK;
 }
-template <typename T>
+template <typename T, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
   switch (lanes_of(P.R.D)) {
-    case 1: return launch_grad<T, 1>(P, dgamma_q, dgamma_k, s);
-    case 2: return launch_grad<T, 2>(P, dgamma_q, dgamma_k, s);
-    case 4: return launch_grad<T, 4>(P, dgamma_q, dgamma_k, s);
-    case 8: return launch_grad<T, 8>(P, dgamma_q, dgamma_k, s);
-    case 16: return launch_grad<T, 16>(P, dgamma_q, dgamma_k, s);
-    default: return launch_grad<T, 32>(P, dgamma_q, dgamma_k, s);
+    case 4: return launch_grad<T, 4, INTER>(P, dgamma_q, dgamma_k, s);
+    case 8: return launch_grad<T, 8, INTER>(P, dgamma_q, dgamma_k, s);
+    case 16: return launch_grad<T, 16, INTER>(P, dgamma_q, dgamma_k, s);
+    default: return launch_grad<T, 32, INTER>(P, dgamma_q, dgamma_k, s);
   }
+}
+template <typename T>
+mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
+  return P.R.inter ? launch_grad<T, true>(P, dgamma_q, dgamma_k, s) : launch_grad<T, false>(P, dgamma_q, dgamma_k, s);
 }
 
 // counts and types that the training calls have in common
@@ -360,7 +382,7 @@ extern "C" mst_status_t mst_qk_norm_rotate_fwd(const mst_rotation_t* rotation, m
   P.Q = Q; P.K = K; P.Qo = Q_out; P.Ko = K_out;
   P.ld = ld; P.ldq = ldo;
   P.hq = heads_q; P.hk = heads_k;
-  P.positions = positions; P.seq_len = seq_len; P.tokens = tokens;
+  P.positions = positions; P.seq_len = seq_len; P.tokens = (int)tokens;
   return dtype == MST_BF16 ? launch_rows<__nv_bfloat16, false>(P, (cudaStream_t)stream) : launch_rows<float, false>(P, (cudaStream_t)stream);
 }
 
@@ -407,7 +429,7 @@ extern "C" mst_status_t mst_qk_norm_rotate_bwd(const mst_rotation_t* rotation, m
   P.dQo = dQ_out; P.dKo = dK_out; P.dQ = dQ; P.dK = dK;
   P.ld = ld; P.lddo = lddo; P.ldg = ldg;
   P.hq = heads_q; P.hk = heads_k;
-  P.positions = positions; P.seq_len = seq_len; P.tokens = tokens;
+  P.positions = positions; P.seq_len = seq_len; P.tokens = (int)tokens;
   P.partial = sums ? (float*)workspace : nullptr;
   if (empty) {   // sums over nothing
     if (dgamma_q) MST_CUDA_TRY(cudaMemsetAsync(dgamma_q, 0, sizeof(float) * P.R.D, (cudaStream_t)stream));

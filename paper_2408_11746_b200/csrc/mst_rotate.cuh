@@ -1,17 +1,21 @@
 // Norm and rotation of one head's row by a group of lanes: shared by the training calls and the append to a paged cache.
 //
-// A row of D = 8 .. 256 values lies in the registers of D / 8 neighbouring lanes, eight values a lane: one 16-byte load (bf16) or two
-// (fp32), and the sum of squares is log2(lanes) shuffles.  With c, s the cosine and sine of a value's angle, and a partner value p,
-//   y = r (x A + p B),   A = gamma c,  B = -/+ gamma_partner s,   r = 1 / sqrt(mean(x^2) + eps)
-// so a row costs two multiply-adds a value once A and B are in registers; they change with the token and the side only (queries, keys),
-// not from head to head.  The partner is in the lane itself (neighbouring pairs) or, raw, one shuffle a word away (halves).
+// A row of D = 8 .. 256 values lies in the registers of G neighbouring lanes, four pairs (u, v) a lane: two runs of four values, `near` and
+// `far` elements into the row.  Where pairs are halves apart the runs are rot / 2 apart, so both values of a pair are in one lane and nothing
+// is exchanged but the sum of squares (log2 G shuffles); neighbouring pairs lie within a run.  Values that do not turn fill further lanes
+// with runs of their own.  Two values that go through the same step share an instruction (f32x2).  With c, s the cosine and sine of the
+// pair's angle and r = 1 / sqrt(mean(x^2) + eps)
+//   u' = r (u gamma_u c - v gamma_v s),   v' = r (u gamma_u s + v gamma_v c)
+// where the products of weights and angles change with the token and the side (queries, keys) only, not from head to head.
 #pragma once
 #include <cuda_bf16.h>
 
 #include "mst_internal.cuh"
 #include "mst_tc_gemm.cuh"
+#include "mst_tc_ptx.cuh"
 
 namespace mst_rot {
+using namespace mst_ptx;
 
 constexpr int WARPS = 8;                    // of a block, each on its own
 constexpr int MAX_HALF = 128;               // rot_dim / 2
@@ -33,63 +37,133 @@ inline mst_status_t check(const mst_rotation_t* r, Rotation* out) {
   *out = Rotation{r->head_dim, r->rot_dim, r->interleaved != 0, r->eps, r->inv_freq, r->gamma_q, r->gamma_k};
   return MST_OK;
 }
-// lanes of a row: the power of two that holds D / 8
-inline int lanes_of(int D) {
-  int g = 1;
-  while (g * 8 < D) g *= 2;
-  return g;
-}
+// lanes of a row: D / 8 of them have values; rows of up to 32 values share a kernel
+inline int lanes_of(int D) { return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
-// ---------------------------------------------------------------------------------------------- eight values of a row
-template <typename T>
-struct Raw {
-  static constexpr int W = sizeof(T) * 2;   // words
-  uint32_t w[W];
+// ---------------------------------------------------------------------------------------------- a lane's part of a row
+struct Lane {
+  int near, far;    // first elements of its two runs
+  bool in, turns;
+  __device__ __forceinline__ Lane(const Rotation& R, int li, bool inter) {
+    in = 8 * li < R.D;
+    turns = 8 * li < R.rot;
+    if (inter) {
+      near = 8 * li;
+      far = near + 4;
+    } else if (turns) {
+      near = 4 * li;
+      far = near + R.rot / 2;
+    } else {
+      near = R.rot + 4 * (li - R.rot / 8);
+      far = near + (R.D - R.rot) / 2;
+    }
+    if (!in) near = far = 0;
+  }
 };
 template <typename T>
-__device__ __forceinline__ Raw<T> load8(const T* p) {
-  Raw<T> r;
+struct Raw {
+  uint32_t w[sizeof(T) * 2];
+};
+__device__ __forceinline__ void load_row(Raw<__nv_bfloat16>& r, const __nv_bfloat16* p, const Lane& L) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p + L.near), b = *reinterpret_cast<const uint2*>(p + L.far);
+  r.w[0] = a.x; r.w[1] = a.y; r.w[2] = b.x; r.w[3] = b.y;
+}
+__device__ __forceinline__ void load_row(Raw<float>& r, const float* p, const Lane& L) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p + L.near), b = *reinterpret_cast<const uint4*>(p + L.far);
+  r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+  r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+}
+__device__ __forceinline__ void store_row(const Raw<__nv_bfloat16>& r, __nv_bfloat16* p, const Lane& L) {
+  *reinterpret_cast<uint2*>(p + L.near) = make_uint2(r.w[0], r.w[1]);
+  *reinterpret_cast<uint2*>(p + L.far) = make_uint2(r.w[2], r.w[3]);
+}
+__device__ __forceinline__ void store_row(const Raw<float>& r, float* p, const Lane& L) {
+  *reinterpret_cast<uint4*>(p + L.near) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+  *reinterpret_cast<uint4*>(p + L.far) = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+}
+template <typename T>
+__device__ __forceinline__ void no_row(Raw<T>& r) {
 #pragma unroll
-  for (int i = 0; i < Raw<T>::W; i += 4) {
-    const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
-    r.w[i] = v.x; r.w[i + 1] = v.y; r.w[i + 2] = v.z; r.w[i + 3] = v.w;
+  for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.w[i] = 0u;
+}
+
+// Four pairs, two to a register pair: u and v hold values 0, 1 and 2, 3
+struct Pairs {
+  uint64_t u[2], v[2];
+};
+// eight values in the order of memory (two runs of four) <-> pairs
+template <bool INTER>
+__device__ __forceinline__ Pairs pairs_of(const float (&x)[8]) {
+  Pairs p;
+  if (INTER) {
+    p.u[0] = pack2(x[0], x[2]); p.v[0] = pack2(x[1], x[3]);
+    p.u[1] = pack2(x[4], x[6]); p.v[1] = pack2(x[5], x[7]);
+  } else {
+    p.u[0] = pack2(x[0], x[1]); p.u[1] = pack2(x[2], x[3]);
+    p.v[0] = pack2(x[4], x[5]); p.v[1] = pack2(x[6], x[7]);
   }
-  return r;
+  return p;
 }
-template <typename T>
-__device__ __forceinline__ Raw<T> zero8() {
-  Raw<T> r;
-#pragma unroll
-  for (int i = 0; i < Raw<T>::W; ++i) r.w[i] = 0u;
-  return r;
+template <bool INTER>
+__device__ __forceinline__ void values_of(const Pairs& p, float (&x)[8]) {
+  if (INTER) {
+    unpack2(p.u[0], x[0], x[2]); unpack2(p.v[0], x[1], x[3]);
+    unpack2(p.u[1], x[4], x[6]); unpack2(p.v[1], x[5], x[7]);
+  } else {
+    unpack2(p.u[0], x[0], x[1]); unpack2(p.u[1], x[2], x[3]);
+    unpack2(p.v[0], x[4], x[5]); unpack2(p.v[1], x[6], x[7]);
+  }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const Raw<T>& r) {
-#pragma unroll
-  for (int i = 0; i < Raw<T>::W; i += 4)
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p) + i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
-}
-__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float (&x)[8]) {
+template <bool INTER>
+__device__ __forceinline__ Pairs widen(const Raw<__nv_bfloat16>& r) {
+  float x[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(r.w[i] << 16);
     x[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
   }
+  return pairs_of<INTER>(x);
 }
-__device__ __forceinline__ void widen(const Raw<float>& r, float (&x)[8]) {
+template <bool INTER>
+__device__ __forceinline__ Pairs widen(const Raw<float>& r) {
+  float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.w[i]);
+  return pairs_of<INTER>(x);
 }
-__device__ __forceinline__ void narrow(const float (&x)[8], Raw<__nv_bfloat16>& r) {
+template <bool INTER>
+__device__ __forceinline__ void narrow(const Pairs& p, Raw<__nv_bfloat16>& r) {
+  float x[8];
+  values_of<INTER>(p, x);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    r.w[i] = *reinterpret_cast<const uint32_t*>(&v);
-  }
+  for (int i = 0; i < 4; ++i) r.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
 }
-__device__ __forceinline__ void narrow(const float (&x)[8], Raw<float>& r) {
+template <bool INTER>
+__device__ __forceinline__ void narrow(const Pairs& p, Raw<float>& r) {
+  float x[8];
+  values_of<INTER>(p, x);
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(x[i]);
+}
+// a lane's norm weights (ones where there is no norm or no value)
+template <bool INTER>
+__device__ __forceinline__ Pairs weights(const float* gamma, const Lane& L) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = 1.f;
+  if (gamma && L.in) {
+    const float4 a = *reinterpret_cast<const float4*>(gamma + L.near), b = *reinterpret_cast<const float4*>(gamma + L.far);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+  return pairs_of<INTER>(x);
+}
+__device__ __forceinline__ float halves_sum(uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+__device__ __forceinline__ float dot(const Pairs& a, const Pairs& b) {
+  return halves_sum(add2(fma2(a.u[0], b.u[0], mul2(a.v[0], b.v[0])), fma2(a.u[1], b.u[1], mul2(a.v[1], b.v[1]))));
 }
 template <int G>
 __device__ __forceinline__ float sum_lanes(float v) {
@@ -99,9 +173,13 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 // ---------------------------------------------------------------------------------------------- the turn
-// Cosines and sines of a position into a warp's own table.  The angle in turns, position * inv_freq / 2 pi, is formed in fp64 and loses its whole
-// part there: 53 bits hold 2^31 turns to 2^-22, and what is left goes to sincospi in fp32.
-__device__ __forceinline__ void angles(float2* table, const Rotation& R, int pos, int lane) {
+// Cosines and sines of a position into a warp's own table, and out of it those of the lane's pairs.  The angle in turns, position * inv_freq /
+// 2 pi, is formed in fp64 and loses its whole part there: 53 bits hold 2^31 turns to 2^-22, and what is left goes to sincospi in fp32.
+struct Turn {
+  uint64_t c[2], s[2];
+};
+template <bool INTER>
+__device__ __forceinline__ Turn turn_of(float2* table, const Rotation& R, const Lane& L, int pos, int lane) {
   __syncwarp();
   for (int i = lane; i < R.rot / 2; i += 32) {
     const double turns = (double)pos * ((double)R.inv_freq[i] * 0.15915494309189533577);
@@ -110,77 +188,18 @@ __device__ __forceinline__ void angles(float2* table, const Rotation& R, int pos
     table[i] = v;
   }
   __syncwarp();
-}
-// What a lane's eight values are turned by: y = c x + s p with p the partner's value
-struct Turn {
-  float c[8], s[8];
-};
-// the place of a lane in its row
-struct Lane {
-  int e0;        // first value
-  int from;      // the lane that holds the partners (halves)
-  bool turns;    // e0 < rot
-  bool first;    // halves: the a of the pairs
-  __device__ __forceinline__ Lane(const Rotation& R, int li, int lane) : e0(8 * li), from(lane), turns(8 * li < R.rot), first(8 * li < R.rot / 2) {
-    if (!R.inter && turns) from = first ? lane + R.rot / 16 : lane - R.rot / 16;
-  }
-};
-__device__ __forceinline__ Turn turn_of(const Rotation& R, const Lane& L, const float2* table, bool back) {
   Turn t;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    t.c[e] = 1.f;
-    t.s[e] = 0.f;
-  }
+  t.c[0] = t.c[1] = pack2(1.f, 1.f);
+  t.s[0] = t.s[1] = 0ULL;
   if (L.turns) {
-    const float flip = back ? -1.f : 1.f;
-    if (R.inter) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 v = table[L.e0 / 2 + e / 2];
-        t.c[e] = v.x;
-        t.s[e] = (e & 1) ? flip * v.y : -flip * v.y;
-      }
-    } else {
-      const int i0 = L.first ? L.e0 : L.e0 - R.rot / 2;
-      const float sign = L.first ? -flip : flip;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 v = table[i0 + e];
-        t.c[e] = v.x;
-        t.s[e] = sign * v.y;
-      }
-    }
+    const float4* at = reinterpret_cast<const float4*>(table + (INTER ? L.near / 2 : L.near));
+    const float4 a = at[0], b = at[1];
+    t.c[0] = pack2(a.x, a.z); t.s[0] = pack2(a.y, a.w);
+    t.c[1] = pack2(b.x, b.z); t.s[1] = pack2(b.y, b.w);
   }
   return t;
 }
-// the partners' values
-template <typename T>
-__device__ __forceinline__ void partners(const Rotation& R, const Lane& L, const Raw<T>& raw, const float (&x)[8], float (&p)[8]) {
-  if (R.inter) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = x[e ^ 1];
-  } else {
-    Raw<T> o;
-#pragma unroll
-    for (int i = 0; i < Raw<T>::W; ++i) o.w[i] = __shfl_sync(0xffffffffu, raw.w[i], L.from);
-    widen(o, p);
-  }
-}
-// A and B of a side: the turn with the weights in it (weights of values beyond D and of no norm: 1)
-__device__ __forceinline__ void weights(const Rotation& R, const Lane& L, const float* gamma, float (&own)[8], float (&partner)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) own[e] = partner[e] = 1.f;
-  if (gamma && L.e0 < R.D) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) own[e] = gamma[L.e0 + e];
-    if (L.turns) {
-      const int at = R.inter ? L.e0 : L.first ? L.e0 + R.rot / 2 : L.e0 - R.rot / 2;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) partner[e] = gamma[R.inter ? at + (e ^ 1) : at + e];
-    }
-  }
-}
+__device__ __forceinline__ uint64_t negated(uint64_t v) { return v ^ 0x8000000080000000ULL; }
 
 // A warp's steps through a token: 32 / G rows each, first the queries', then the keys', then the values' (which are only carried along).
 struct Steps {
@@ -189,10 +208,12 @@ struct Steps {
   __host__ __device__ int all() const { return q + k + v; }
 };
 // Tokens alone fill the GPU from some thousands on; below that a token's steps are shared out, so that a few tokens are not a few warps' long
-// chains of loads.
-inline int warps_of_token(int64_t tokens, int steps) {
-  const int64_t want = (int64_t)mst_sm_count() * 32 / (tokens > 0 ? tokens : 1);
-  return want <= 1 ? 1 : want >= steps ? (steps > 0 ? steps : 1) : (int)want;
+// chains of loads.  Returns the warps of a token and sets their steps.
+inline int share_token(int64_t tokens, int steps, int* per_warp) {
+  const int64_t want = (int64_t)mst_sm_count() * 24 / (tokens > 0 ? tokens : 1);
+  const int warps = want <= 1 ? 1 : want >= steps ? steps : (int)want;
+  *per_warp = (steps + warps - 1) / warps;
+  return (steps + *per_warp - 1) / *per_warp;
 }
 
 }  // namespace mst_rot

@@ -193,6 +193,21 @@ def test_extreme_rows():
     np.testing.assert_allclose(y[2, :2], ref[0], rtol=0.01, atol=0.01)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [0, 32])
+def test_values_that_do_not_turn_stay_on_their_own(rot, interleaved):
+    c = Case(5, 2, 1, 64, rot, interleaved, norm="")
+    x, dy = c.x.clone(), c.dy.clone()
+    x[1, 40], x[2, 64 + 63], dy[3, 50] = float("inf"), float("nan"), float("-inf")
+    y, dx = c.padded(), c.padded()
+    c.forward(c.padded(x), y)
+    c.backward(c.padded(x), c.padded(dy), dx)
+    torch.cuda.synchronize()
+    y, dx = host(y), host(dx)
+    assert np.isinf(y[1, 40]) and np.isnan(y[2, 127]) and np.isinf(dx[3, 50])
+    assert np.isfinite(y).sum() == y.size - 2 and np.isfinite(dx).sum() == dx.size - 1
+
+
 def test_streams_and_a_captured_graph():
     c = Case(200, 12, 12, 64, 64)
     x, dy = c.padded(c.x), c.padded(c.dy)
