@@ -234,6 +234,7 @@ mst_status_t mst_attention_error_flags(int32_t* flags);
 mst_status_t mst_attention_bwd_error_flags(int32_t* flags);
 // bit 0: pages that do not exist were named (cleared by this call), bit 1: bounded waits (mst_paged_attention.cu); the append's bit 0 (mst_rotate.cu)
 mst_status_t mst_paged_error_flags(int32_t* flags);
+mst_status_t mst_paged_tiles_error_flags(int32_t* flags);
 mst_status_t mst_append_error_flags(int32_t* flags);
 
 // bins of one radix-select pass (digit width MST_SELECT_RADIX_BITS)

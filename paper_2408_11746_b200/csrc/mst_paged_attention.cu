@@ -2,111 +2,16 @@
 //   Out = sum_{j in S_i} softmax_j(q . k_j / sqrt(d)) v_j,   S_i = { j <= i : i - j < l  or  (i - j) mod l == 0 }.
 // Tiles of rows and the lists of keys they look at: mst_paged_list.h.  Few rows (one token, drafts): paged_rows_kernel, a block per (tile, key head,
 // sequence, range of the list).
-#include <cuda_bf16.h>
-
-#include "mst_attention_tile.cuh"
-#include "mst_internal.cuh"
-#include "mst_paged.cuh"
+#include "mst_paged_attention.cuh"
 
 namespace {
-using namespace mst_ptx;
-using mst_att::ex2;
+using namespace mst_paged;
 using mst_att::ldsm_x4;
 using mst_att::ldsm_x4_t;
 using mst_att::mma_bf16;
-using mst_paged::Batch;
-using mst_paged::Cache;
-using mst_paged::Key;
-using mst_paged::List;
 
-__device__ int g_bad_page = 0;
-
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float LAZY = 16.f;     // the reference of a softmax follows the maximum once that has moved up by 2^16: fp32 sums and bf16 weights lose nothing by it
-
-struct Params {
-  Cache C;
-  Batch B;
-  const __nv_bfloat16* Q;
-  __nv_bfloat16* Out;
-  float* lse;
-  int64_t ldq, ldo;
-  int heads, group, l;
-  float scale_log2;
-  int splits, least;      // most ranges of a list, and the least units of one (plan)
-  float* part_o;          // [splits][tokens * heads][D]: sums against part_m, [splits][tokens * heads][2]: reference and sum of weights
-  float* part_m;
-};
-
-constexpr int UNIT = 64;  // keys of a list that stay together
-
-// A tile of sequence b (mst_paged_list.h)
-__device__ __forceinline__ bool locate(List& T, const Params& P, int b, int tile, int R) {
-  const int len = P.B.len[b];
-  const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.group, P.l, reach, tile, R)) return false;
-  if (len > reach) g_bad_page = 1;
-  return true;
-}
-
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-// A row's sums -> its result, by one warp (lane: E neighbouring columns).  Nothing looked at: zeros and -inf
-template <int E>
-__device__ __forceinline__ void finish(const Params& P, int64_t token, int h, int lane, const float (&o)[E], float m, float sum) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint32_t w[E / 2];
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-  uint32_t* out = reinterpret_cast<uint32_t*>(P.Out + token * P.ldo + (int64_t)h * (32 * E)) + lane * (E / 2);
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) out[e] = w[e];
-  if (P.lse && lane == 0) P.lse[(int64_t)h * P.B.tokens + token] = (m + log2f(sum)) * LN2;
-}
-
-// A row whose sums are not finite, formed again by one warp over the entries it looks at alone: what the matrix products multiplied by a weight
-// of zero may have been infinite or NaN.  Lane: D / 32 neighbouring columns.
-template <int D>
-__device__ __noinline__ void row_again(const Params& P, const List T, int b, int kvh, int row, uint32_t lo, uint32_t hi, float (&o)[D / 32], float& m,
-                                       float& sum) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int t = (T.row0 + row) / P.group, h = kvh * P.group + (T.row0 + row) % P.group;
-  const __nv_bfloat16* q = P.Q + (int64_t)(T.first + t) * P.ldq + (int64_t)h * D + lane * E;
-  m = -INFINITY;
-  sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (uint32_t n = lo; n < hi; ++n) {
-    const Key k = T.key(n);
-    if (!T.sees(T.p_lo + t - T.t_lo, t - T.t_lo, k)) continue;
-    const mst_paged::Slot s = mst_paged::slot_of(P.C, P.B, b, k.pos, &g_bad_page);
-    if (!s.exists) continue;
-    const int64_t at = s.at + (int64_t)kvh * P.C.head_stride + lane * E;
-    float x = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x = fmaf(__bfloat162float(q[e]), __bfloat162float(P.C.K[at + e]), x);
-    x = warp_sum(x) * P.scale_log2;
-    const float up = fmaxf(m, x);        // NaN: the weight below is NaN all the same
-    const float c = ex2(m - reference(up)), w = ex2(x - reference(up));
-    m = up;
-    sum = fmaf(sum, c, w);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, w * __bfloat162float(P.C.V[at + e]));
-  }
-}
+// how many entries below `f` of the list behind the window are token `t`'s of `nt`
+__device__ __forceinline__ uint32_t steps_below(uint32_t f, uint32_t t, uint32_t nt) { return f > t ? (f - t - 1) / nt + 1 : 0u; }
 
 // ---------------------------------------------------------------------------------------------- few rows
 // Four warps go through a range of the list, each through every fourth step of it with a ring of its own (no block-wide step until the
@@ -180,7 +85,7 @@ __global__ void __launch_bounds__(32 * RW) paged_rows_kernel(const __grid_consta
       next = n < hi ? T.key((uint32_t)n) : Key{-1, -1};
       next_at = 0;
       if (next.pos >= 0) {
-        const mst_paged::Slot sl = mst_paged::slot_of(P.C, P.B, b, next.pos, &g_bad_page);
+        const Slot sl = slot_of(P.C, P.B, b, next.pos, &g_bad_page);
         if (sl.exists) next_at = sl.at + (int64_t)kvh * P.C.head_stride;
         else next.pos = -1;
       }
@@ -350,7 +255,12 @@ __global__ void __launch_bounds__(32 * RW) paged_rows_kernel(const __grid_consta
       bool bad = !(total_w * 0.f == 0.f);
 #pragma unroll
       for (int e = 0; e < E; ++e) bad = bad || !(o[e] * 0.f == 0.f);
-      if (__any_sync(0xffffffffu, bad)) row_again<D>(P, T, b, kvh, r, lo, hi, o, mm, total_w);
+      if (__any_sync(0xffffffffu, bad)) {
+        const uint32_t w_lo = lo < T.W ? lo : T.W, w_hi = hi < T.W ? hi : T.W, f_lo = lo - w_lo, f_hi = hi - w_hi;   // of the window, behind it
+        const uint32_t t_in = (uint32_t)((T.row0 + r) / P.group - T.t_lo), nt = (uint32_t)T.nt;
+        row_again<D>(P, T, b, kvh, r, T.w0 + (int)w_lo, T.w0 + (int)w_hi, T.l - 1, 1 + (int)steps_below(f_lo, t_in, nt), 1 + (int)steps_below(f_hi, t_in, nt),
+                     o, mm, total_w);
+      }
       const int t = (T.row0 + r) / P.group, h = kvh * P.group + (T.row0 + r) % P.group;
       const int64_t token = T.first + t;
       if (active == 1) {
@@ -370,60 +280,71 @@ __global__ void __launch_bounds__(32 * RW) paged_rows_kernel(const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------- ranges that meet
-// a warp a row: the ranges' sums against the largest of their references
-template <int D, int R>
-__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ Params P) {
+// a warp a row: the ranges' sums against the largest of their references.  How many ranges a row's list has is worked out as the first launch did
+template <int D, bool TILES>
+__global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__ Params P, int tile_rows) {
   constexpr int E = D / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
-  const int b = blockIdx.z, kvh = blockIdx.y % P.C.kv_heads;
-  for (int tile = blockIdx.y / P.C.kv_heads;; tile += gridDim.y / P.C.kv_heads) {
-    List T;
-    if (!locate(T, P, b, tile, R)) return;
+  const int64_t row = (int64_t)blockIdx.x * 4 + warp, token = row / P.heads;
+  if (token >= P.B.tokens) return;
+  const int h = (int)(row - token * P.heads), b = sequence_of(P.B, (int)token, lane);
+  if (b < 0) return;
+  const int64_t pair = (token - P.B.first[b]) * P.group + h % P.group;
+  List T;
+  if (!locate(T, P, b, (int)(pair / tile_rows), tile_rows)) return;
+  int active;
+  if (TILES) {
+    int n0, n1, m0, m1;
+    TileWalk(T, (int64_t)P.B.table_stride * P.C.page_size).range(P.splits, P.least, 0, n0, n1, m0, m1, active);
+  } else {
     uint32_t lo, hi;
-    int active;
     T.range(P.splits, P.least, UNIT, 0, lo, hi, active);
-    if (active == 1) continue;
-    for (int r = blockIdx.x * 4 + warp; r < T.rows; r += 4 * gridDim.x) {
-      const int t = (T.row0 + r) / P.group, h = kvh * P.group + (T.row0 + r) % P.group;
-      const int64_t token = T.first + t, step = (int64_t)P.B.tokens * P.heads, at = token * P.heads + h;
-      float mm = -INFINITY;
-      for (int s = 0; s < active; ++s) mm = fmaxf(mm, P.part_m[(at + s * step) * 2]);
-      float sum = 0.f, o[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = 0.f;
-      for (int s = 0; s < active; ++s) {
-        const float c = ex2(P.part_m[(at + s * step) * 2] - reference(mm));
-        sum = fmaf(c, P.part_m[(at + s * step) * 2 + 1], sum);
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(c, P.part_o[(at + s * step) * D + lane * E + e], o[e]);
-      }
-      finish<E>(P, token, h, lane, o, mm, sum);
-    }
   }
+  if (active == 1) return;
+  const int64_t step = (int64_t)P.B.tokens * P.heads, at = token * P.heads + h;
+  float mm = -INFINITY;
+#pragma unroll 4
+  for (int s = 0; s < active; ++s) mm = fmaxf(mm, P.part_m[(at + s * step) * 2]);
+  float sum = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < active; ++s) {
+    const float c = ex2(P.part_m[(at + s * step) * 2] - reference(mm));
+    sum = fmaf(c, P.part_m[(at + s * step) * 2 + 1], sum);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(c, P.part_o[(at + s * step) * D + lane * E + e], o[e]);
+  }
+  finish<E>(P, token, h, lane, o, mm, sum);
 }
 
 // ---------------------------------------------------------------------------------------------- the call
-struct Plan {
-  int rows;           // of a tile
-  int tiles, splits, least;
-};
+constexpr int TILE_ROWS = 128, TILES_FROM = 33;
 Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, int stride) {
   Plan p;
   const int group = heads / c.kv_heads;
-  const int64_t rows = (int64_t)(b.max_new > 0 ? b.max_new : 1) * group;
-  p.rows = rows <= 16 ? 16 : 32;
-  int64_t tiles = (rows + p.rows - 1) / p.rows;
-  const int64_t most = 65535 / c.kv_heads;
-  p.tiles = (int)(tiles < most ? tiles : most);
-  // entries of the longest list
-  const int64_t nt = (p.rows + group - 1) / group, len = b.max_len > 0 ? b.max_len : 1;
-  const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
-  const int64_t blocks = (int64_t)(b.batch > 0 ? b.batch : 1) * c.kv_heads * tiles, want = 12 * (int64_t)mst_sm_count();
+  const int64_t rows = (int64_t)(b.max_new > 0 ? b.max_new : 1) * group, len = b.max_len > 0 ? b.max_len : 1;
+  const int64_t lists = (int64_t)(b.batch > 0 ? b.batch : 1) * c.kv_heads;
+  p.tiles = rows >= TILES_FROM && group <= TILE_ROWS && (int64_t)c.kv_heads * 64 < 0x7FFFFFFF;
+  p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 16 ? 16 : 32;
+  const int64_t tiles = (rows + p.rows - 1) / p.rows, most = p.tiles ? 65535 : 65535 / c.kv_heads;
+  p.count = (int)(tiles < most ? tiles : most);
+  // units of the longest list: 64 entries, or tiles of 64 keys
+  const int64_t nt = (p.rows + group - 1) / group;
+  int64_t units;
+  if (p.tiles) {
+    units = (stride >= len ? len : stride + nt < len ? stride + nt : len) / UNIT + 1;
+    p.least = 16;
+  } else {
+    const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
+    units = (list + UNIT - 1) / UNIT;
+    p.least = 4;
+  }
+  const int64_t blocks = lists * tiles, want = (p.tiles ? 8 : 12) * (int64_t)mst_sm_count();
   int64_t splits = (want + blocks - 1) / blocks;
-  p.least = 4;
-  const int64_t units = (list + UNIT - 1) / UNIT, fit = (units + p.least - 1) / p.least;
+  const int64_t fit = (units + p.least - 1) / p.least;
   if (splits > fit) splits = fit;
   if (splits > 64) splits = 64;
   if (splits < 1) splits = 1;
@@ -441,14 +362,20 @@ template <int D, int MT>
 mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
   const size_t smem = RowsShape<D>::SMEM;
   MST_SMEM_LIMIT((paged_rows_kernel<D, MT>), smem);
-  const unsigned y = (unsigned)(plan.tiles * P.C.kv_heads), z = (unsigned)P.B.batch;
+  const unsigned y = (unsigned)(plan.count * P.C.kv_heads), z = (unsigned)P.B.batch;
   MST_CUDA_TRY(mst_launch_overlapped(paged_rows_kernel<D, MT>, dim3((unsigned)plan.splits, y, z), dim3(32 * RW), smem, s, P));
-  if (plan.splits > 1) MST_CUDA_TRY(mst_launch_overlapped(paged_join_kernel<D, 16 * MT>, dim3(4 * MT, y, z), dim3(128), 0, s, P));
+  return MST_OK;
+}
+template <int D>
+mst_status_t launch_join(const Params& P, const Plan& plan, cudaStream_t s) {
+  const unsigned blocks = (unsigned)(((int64_t)P.B.tokens * P.heads + 3) / 4);
+  MST_CUDA_TRY(plan.tiles ? mst_launch_overlapped(paged_join_kernel<D, true>, dim3(blocks), dim3(128), 0, s, P, plan.rows)
+                          : mst_launch_overlapped(paged_join_kernel<D, false>, dim3(blocks), dim3(128), 0, s, P, plan.rows));
   return MST_OK;
 }
 
 mst_status_t check_attention(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, int32_t heads, int32_t stride, Cache* C, Batch* B) {
-  MST_TRY(mst_paged::check(cache, batch, C, B));
+  MST_TRY(check(cache, batch, C, B));
   if (heads <= 0 || stride <= 0) return MST_ERR_INVALID_ARG;
   if (heads % cache->kv_heads != 0 || heads > 65535) return MST_ERR_SHAPE;
   if (cache->head_dim != 64 && cache->head_dim != 128) return MST_ERR_SHAPE;
@@ -457,7 +384,13 @@ mst_status_t check_attention(const mst_paged_cache_t* cache, const mst_paged_bat
 
 }  // namespace
 
-mst_status_t mst_paged_error_flags(int32_t* flags) { return mst_paged::take_flag((const void*)&g_bad_page, flags); }
+mst_status_t mst_paged_error_flags(int32_t* flags) {
+  int32_t rows = 0, tiles = 0;
+  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_page, &rows));
+  MST_TRY(mst_paged_tiles_error_flags(&tiles));
+  *flags = rows | tiles;
+  return MST_OK;
+}
 
 extern "C" mst_status_t mst_paged_attention_workspace(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, int32_t heads,
                                                       int32_t stride, size_t* bytes) {
@@ -502,6 +435,9 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   P.part_o = (float*)workspace;
   if (need) P.part_m = P.part_o + (size_t)plan.splits * (size_t)batch->tokens * (size_t)heads * (size_t)cache->head_dim;
   cudaStream_t s = (cudaStream_t)stream;
-  if (cache->head_dim == 64) return plan.rows == 16 ? launch_rows<64, 1>(P, plan, s) : launch_rows<64, 2>(P, plan, s);
-  return plan.rows == 16 ? launch_rows<128, 1>(P, plan, s) : launch_rows<128, 2>(P, plan, s);
+  if (plan.tiles) MST_TRY(launch_tiles(P, plan, s));
+  else if (cache->head_dim == 64) MST_TRY(plan.rows == 16 ? (launch_rows<64, 1>(P, plan, s)) : (launch_rows<64, 2>(P, plan, s)));
+  else MST_TRY(plan.rows == 16 ? (launch_rows<128, 1>(P, plan, s)) : (launch_rows<128, 2>(P, plan, s)));
+  if (plan.splits > 1) MST_TRY(cache->head_dim == 64 ? launch_join<64>(P, plan, s) : launch_join<128>(P, plan, s));
+  return MST_OK;
 }

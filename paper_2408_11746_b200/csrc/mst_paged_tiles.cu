@@ -1,0 +1,647 @@
+// Attention over a paged cache for many rows (chunks of prompts): tiles of up to 128 (token, head) rows of one key head on the tensor cores.
+// Keys come in tiles of 64 positions (mst_paged_list.h: TileWalk); the strided keys further back, which one row each looks at, are formed row by
+// row and are where the first half's softmax starts.  Roles of a block's ten warps:
+//   warps 0-7  softmax: thread = row (tensor-memory lane), the two warps of a lane quarter take 32 of a tile's 64 keys each, as softmaxes of
+//              their own - reference, sum and output accumulator - that meet when the rows leave;
+//   warp 8     fills a four-slot ring: pages whose positions fall on whole boxes by TMA, one box a page and tile at most 64 rows high; the tile
+//              in which a sequence ends, pages that do not exist and page sizes without a factor of eight by 16-byte asynchronous copies, zeros
+//              where nothing is (what a page holds behind the length may be no number).  Which of a tile's keys exist goes with the slot;
+//   warp 9     one lane issues tcgen05.mma: S = Q K^T (128 x 64) two tiles ahead, O_half += P V over the half's 32 keys, P read from tensor
+//              memory where the softmax warps have written it over the scores.
+// Tensor memory: scores in columns 0-63 and 64-127, the halves' outputs behind.  Ranges of a list (blockIdx.x) leave sums for the join.
+// Bound: exponentials (16 a clock and SM: 512 clocks a 128 x 64 tile, the products need 256), two blocks an SM at head_dim 64.
+#include <cuda.h>
+
+#include "mst_paged_attention.cuh"
+
+namespace {
+using namespace mst_paged;
+using namespace mst_att;
+using mst_ptx::pack_bf16;
+
+__device__ int g_wait_error = 0;
+
+constexpr int STAGES = 4;
+constexpr int LAG = 2;            // tiles of plain copies under way before the oldest is waited for
+template <int D_>
+struct Shape {
+  static constexpr int PARTS = D_ / 64;                            // 64 columns each: 128 bytes a row
+  static constexpr int OWN_BYTES = PARTS * 2 * TILE_BYTES;
+  static constexpr int STAGE_BYTES = PARTS * 2 * TILE_BYTES;       // keys, then values
+  static constexpr int TMEM_COLS = D_ == 64 ? 256 : 512;
+  static constexpr int BLOCKS = D_ == 64 ? 2 : 1;
+  // own rows, ring, statistics, which keys exist, barriers (full, empty, own_full, s_full[2], p_full[2], o_done, acc_full, far_over)
+  static constexpr int SMEM = OWN_BYTES + STAGES * STAGE_BYTES + 3 * 2 * ROWS * 4 + STAGES * 8 + 16 * STAGES + 8 * 8 + 1024;
+};
+
+struct TileParams {
+  Params P;
+  int rows;             // of a tile: whole tokens
+  int count;            // tiles of a sequence that the grid has
+  int box;              // rows of a TMA box, 0: plain copies only
+  int at_slot, at_head, at_page;   // which of the map's coordinates 1 .. 3 they are
+};
+
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_wait(bar, parity, abort_flag, &g_wait_error);
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(tm),
+               "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void softmax_warps_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// ---------------------------------------------------------------------------------------------- strided keys of a row
+// Two lanes a row, D / 2 columns each, from the caller's memory
+template <int W>
+struct Half {
+  uint32_t w[W];      // W pairs of values
+};
+template <int W>
+__device__ __forceinline__ void half_row(Half<W>& x, const __nv_bfloat16* p, bool there) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (there) v = *reinterpret_cast<const uint4*>(p + 2 * i);
+    x.w[i] = v.x; x.w[i + 1] = v.y; x.w[i + 2] = v.z; x.w[i + 3] = v.w;
+  }
+}
+template <int W>
+__device__ __forceinline__ float half_dot(const Half<W>& a, const Half<W>& b) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    uint16_t al, ah, bl, bh;
+    halves(a.w[e], al, ah);
+    halves(b.w[e], bl, bh);
+    fma_bf16(s[e & 1], al, bl);
+    fma_bf16(s[2 + (e & 1)], ah, bh);
+  }
+  const float x = (s[0] + s[1]) + (s[2] + s[3]);
+  return x + __shfl_xor_sync(0xffffffffu, x, 16);
+}
+// the sums of sixteen rows -> tensor memory from lane rs on: lanes 0-15 of the warp hold columns 0 .. D / 2 - 1, lanes 16-31 the others
+__device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[32]) { far_start_sums(taddr, a); }
+__device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[64]) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x32bx2.x32.b32 [%32], 64, "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"f"(a[32 * g + 0]),
+        "f"(a[32 * g + 1]), "f"(a[32 * g + 2]), "f"(a[32 * g + 3]), "f"(a[32 * g + 4]), "f"(a[32 * g + 5]), "f"(a[32 * g + 6]), "f"(a[32 * g + 7]),
+        "f"(a[32 * g + 8]), "f"(a[32 * g + 9]), "f"(a[32 * g + 10]), "f"(a[32 * g + 11]), "f"(a[32 * g + 12]), "f"(a[32 * g + 13]),
+        "f"(a[32 * g + 14]), "f"(a[32 * g + 15]), "f"(a[32 * g + 16]), "f"(a[32 * g + 17]), "f"(a[32 * g + 18]), "f"(a[32 * g + 19]),
+        "f"(a[32 * g + 20]), "f"(a[32 * g + 21]), "f"(a[32 * g + 22]), "f"(a[32 * g + 23]), "f"(a[32 * g + 24]), "f"(a[32 * g + 25]),
+        "f"(a[32 * g + 26]), "f"(a[32 * g + 27]), "f"(a[32 * g + 28]), "f"(a[32 * g + 29]), "f"(a[32 * g + 30]), "f"(a[32 * g + 31]),
+        "r"(taddr + 32u * g)
+        : "memory");
+}
+
+template <int D_>
+__global__ void __launch_bounds__(THREADS, Shape<D_>::BLOCKS)
+paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ TileParams A) {
+  using S = Shape<D_>;
+  constexpr int PARTS = S::PARTS, HALF = D_ / 2, OUT0 = 128;     // OUT0: tensor-memory column of the first half's outputs
+  const Params& P = A.P;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t own = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = own + S::OWN_BYTES, stat_a = ring + STAGES * S::STAGE_BYTES;
+  const uint32_t exist_a = stat_a + 3 * 2 * ROWS * 4, full = exist_a + 8 * STAGES, empty = full + 8 * STAGES, own_full = empty + 8 * STAGES,
+                 s_full = own_full + 8, p_full = s_full + 16, o_done = p_full + 16, acc_full = o_done + 8, far_over = acc_full + 8;
+  unsigned char* base = smem_raw + (own - smem_u32(smem_raw));
+  volatile unsigned long long* exist = reinterpret_cast<unsigned long long*>(base + (exist_a - own));
+  __shared__ uint32_t holder;
+  __shared__ uint32_t again[ROWS / 32];
+  __shared__ int abort_sh;
+  volatile int* abort_flag = &abort_sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    abort_sh = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    mbar_init(own_full, 1);
+    for (int e = 0; e < 2; ++e) {
+      mbar_init(s_full + 8 * e, 1);
+      mbar_init(p_full + 8 * e, CW);
+    }
+    mbar_init(o_done, 1);
+    mbar_init(acc_full, 1);
+    mbar_init(far_over, CW);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x < ROWS / 32) again[threadIdx.x] = 0u;
+  if (warp == CW && lane < 3) prefetch_map(lane == 0 ? &tmQ : lane == 1 ? &tmK : &tmV);
+  if (warp == CW + 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&holder)), "r"(S::TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = holder;
+  mst_grid_launch_dependents();
+  mst_grid_dependency_wait();
+
+  const int kvh = (int)blockIdx.x % P.C.kv_heads, split = (int)blockIdx.x / P.C.kv_heads, b = (int)blockIdx.y;
+  const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
+  const int len = P.B.len[b], have = (int)(len < reach ? len : reach);       // positions that there are
+  // late tiles have the most keys and come first
+  const int64_t all = P.B.first[b + 1] > P.B.first[b] ? ((int64_t)P.B.first[b + 1] - P.B.first[b]) * P.group : 0;
+  const int tiles = (int)((all + A.rows - 1) / A.rows);
+  uint32_t lap = 0, far_lap = 0;   // tiles of rows so far, those with strided keys: barriers that complete once in each
+  uint32_t base_t = 0;  // near tiles so far: ring places and score buffers go on from tile to tile
+  bool ok = true;
+  for (int z = (int)blockIdx.z; z < tiles; z += A.count) {
+    List T;
+    if (!locate(T, P, b, tiles - 1 - z, A.rows)) break;
+    const TileWalk walk(T, reach);
+    int n0, n1, m0, m1, active;
+    if (!walk.range(P.splits, P.least, split, n0, n1, m0, m1, active)) continue;
+    const int near = n1 - n0, key0 = walk.first + n0 * TS;
+    if (near == 0) {      // no row has a position
+      if (warp < CW)
+        for (int r = warp; r < T.rows; r += CW) {
+          const float none[D_ / 32] = {};
+          finish<D_ / 32>(P, T.first + (T.row0 + r) / P.group, kvh * P.group + (T.row0 + r) % P.group, lane, none, -INFINITY, 0.f);
+        }
+      continue;
+    }
+    if (warp == CW) {
+      // ------------------------------------------------------------------------------------------ loads
+      if (lane == 0) {
+        mbar_expect_tx(own_full, (uint32_t)(A.rows * D_ * 2));
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c)
+          tma_load_3d(own + c * 2 * TILE_BYTES, &tmQ, 64 * c, kvh * P.group, T.first + T.t_lo, own_full);
+      }
+      int waiting = 0;       // tiles of plain copies whose slots have not been given out
+      uint32_t oldest = 0;
+      auto give = [&]() {
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full + 8 * (oldest % STAGES));
+        ++oldest;
+        --waiting;
+      };
+      const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
+      for (int j = 0; j < near && ok; ++j) {
+        const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
+        const int k0 = key0 + j * TS;
+        const uint32_t dst = ring + s * S::STAGE_BYTES, bar = full + 8 * s;
+        bool whole = A.box > 0 && k0 + TS <= have;
+        int id = 0, slot = 0;
+        const bool mine = whole && lane * A.box < TS;
+        if (mine) id = page_of(table, P.B.table_stride, P.C.page_size, P.C.num_pages, k0 + lane * A.box, slot);
+        whole = whole && __all_sync(0xffffffffu, id >= 0);
+        if (whole)
+          while (waiting > 0) {
+            cp_wait<0>();
+            give();
+          }
+        if (n >= STAGES) ok = wait_on(empty + 8 * s, (n / STAGES - 1) & 1u, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (whole) {
+          if (lane == 0) {
+            exist[s] = ~0ULL;
+            mbar_expect_tx(bar, S::STAGE_BYTES);
+          }
+          __syncwarp();
+          if (mine) {
+            int c[4];
+#pragma unroll
+            for (int d = 1; d < 4; ++d) c[d] = d == A.at_slot ? slot : d == A.at_head ? kvh : id;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) {
+              const uint32_t to = dst + (uint32_t)(q * TILE_BYTES + lane * A.box * 128);
+              tma_load_4d(to, &tmK, 64 * q, c[1], c[2], c[3], bar);
+              tma_load_4d(to + PARTS * TILE_BYTES, &tmV, 64 * q, c[1], c[2], c[3], bar);
+            }
+          }
+        } else {
+          if (waiting == 0) oldest = n;
+          int64_t at[2];
+          bool there[2];
+          unsigned long long bits = 0ULL;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int k = k0 + 32 * u + lane;
+            at[u] = 0;
+            there[u] = false;
+            if (k < have) {
+              const Slot sl = slot_of(P.C, P.B, b, k, &g_bad_page);
+              there[u] = sl.exists;
+              if (sl.exists) at[u] = sl.at + (int64_t)kvh * P.C.head_stride;
+            }
+            bits |= (unsigned long long)__ballot_sync(0xffffffffu, there[u]) << (32 * u);
+          }
+          if (lane == 0) exist[s] = bits;
+          constexpr int PIECES = D_ / 8, AT_ONCE = 32 / PIECES;
+          const int c = lane % PIECES;
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll 4
+            for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+              const int r = r0 + lane / PIECES;
+              const int64_t a = __shfl_sync(0xffffffffu, at[u], r);
+              const bool in = __shfl_sync(0xffffffffu, there[u], r);
+              const uint32_t to = piece_addr(dst + (uint32_t)(c / 8) * TILE_BYTES, 32 * u + r, c % 8);
+              cp16(to, P.C.K + a + c * 8, in);
+              cp16(to + PARTS * TILE_BYTES, P.C.V + a + c * 8, in);
+            }
+          cp_commit();
+          ++waiting;
+          if (waiting > LAG) {
+            cp_wait<LAG>();
+            give();
+          }
+        }
+      }
+      while (waiting > 0 && ok) {
+        cp_wait<0>();
+        give();
+      }
+      cp_wait<0>();
+      ok = __all_sync(0xffffffffu, ok);
+    } else if (warp == CW + 1) {
+      // ------------------------------------------------------------------------------------------ products
+      if (lane == 0) {
+        const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring, 16, 1024);
+        const uint64_t step = S::STAGE_BYTES >> 4, part = TILE_BYTES >> 4;
+        const uint32_t from_far = m1 > m0 ? 1u : 0u;
+        auto scores = [&](int j) {
+          const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
+          if (!wait_on(full + 8 * s, (n / STAGES) & 1u, abort_flag)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              tc_mma(tmem + (n & 1u) * 64u, qd + 2 * part * q + 2 * ks, kd0 + step * s + part * q + 2 * ks, IDESC_K, (q > 0 || ks > 0) ? 1u : 0u);
+          tc_commit(s_full + 8 * (n & 1u));
+          return true;
+        };
+        ok = wait_on(own_full, lap & 1u, abort_flag);
+        ok = ok && scores(0);
+        if (ok && near > 1) ok = scores(1);
+        if (ok && from_far) {
+          ok = wait_on(far_over, far_lap & 1u, abort_flag);
+          tc_fence_after();
+        }
+        for (int j = 0; j < near && ok; ++j) {
+          const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
+          ok = wait_on(p_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t p = tmem + (n & 1u) * 64u;
+          const uint64_t vd = kd0 + step * s + part * PARTS;
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)   // 16 keys each: two of the first half's 32, two of the second's
+              tc_mma_ts(tmem + OUT0 + (uint32_t)((ks >> 1) * D_ + 64 * q), p + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8),
+                        vd + part * q + (uint64_t)(ks * ((16 * 128) >> 4)), IDESC_MN, (j > 0 || (ks & 1)) ? 1u : ks == 0 ? from_far : 0u);
+          tc_commit(empty + 8 * s);
+          tc_commit(o_done);
+          if (j + 1 == near) tc_commit(acc_full);
+          if (j + 2 < near) ok = scores(j + 2);
+        }
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    } else {
+      // ------------------------------------------------------------------------------------------ softmax
+      const int quarter = warp & 3, half = warp >> 2;
+      const int r = quarter * 32 + lane, rs = quarter * 32 + half * 16;   // this thread's row; this warp's sixteen of the strided keys
+      const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16), t_out = t_row + OUT0 + (uint32_t)half * D_;
+      const uint64_t scale2 = pack2(P.scale_log2, P.scale_log2);
+      float* stat = reinterpret_cast<float*>(base + (stat_a - own));      // [3][2][128]
+      const bool live = r < T.rows;
+      const int pos = live ? T.p_lo + (T.row0 + r) / P.group - T.t_lo : -1;
+      const int w0 = quarter * 32, w1 = w0 + 31 < T.rows ? w0 + 31 : T.rows - 1;     // this warp's rows
+      const int i_lo = T.p_lo + (T.row0 + w0) / P.group - T.t_lo, i_hi = w0 < T.rows ? T.p_lo + (T.row0 + w1) / P.group - T.t_lo : -1;
+      float m = -INFINITY;                                   // reference of this half's softmax, base 2
+      uint64_t sum2 = 0ULL;
+      if (m1 > m0) {
+        const int fr = rs + (lane & 15);
+        const bool there = fr < T.rows;
+        const int fp = there ? T.p_lo + (T.row0 + fr) / P.group - T.t_lo : -1;
+        const int col = (lane >> 4) * HALF;
+        Half<HALF / 2> mine;
+        half_row(mine, P.Q + (int64_t)(T.first + (there ? (T.row0 + fr) / P.group : 0)) * P.ldq + (int64_t)(kvh * P.group + (there ? (T.row0 + fr) % P.group : 0)) * D_ + col, there);
+        float acc[HALF], fm = -INFINITY, fs = 0.f;
+#pragma unroll
+        for (int e = 0; e < HALF; ++e) acc[e] = 0.f;
+        for (int k = m0; k < m1; ++k) {
+          const int64_t j = (int64_t)fp - (int64_t)k * P.l;
+          Slot sl = {false, 0};
+          if (j >= 0) sl = slot_of(P.C, P.B, b, (int)j, &g_bad_page);
+          const int64_t at = sl.at + (int64_t)kvh * P.C.head_stride + col;
+          Half<HALF / 2> kk, vv;
+          half_row(kk, P.C.K + at, sl.exists);
+          half_row(vv, P.C.V + at, sl.exists);
+          const float d = half_dot(mine, kk);          // every lane: it has a shuffle
+          const float x = sl.exists ? d * P.scale_log2 : -INFINITY;
+          const bool up = x > fm + LAZY;
+          if (__any_sync(0xffffffffu, up)) {
+            const float c = up ? ex2(fm - x) : 1.f;
+            if (up) fm = x;
+            fs *= c;
+#pragma unroll
+            for (int e = 0; e < HALF; ++e) acc[e] *= c;
+          }
+          const float w = sl.exists ? ex2(x - mst_paged::reference(fm)) : 0.f;
+          fs += w;
+          uint16_t wb, dummy;
+          halves(pack_bf16(w, 0.f), wb, dummy);
+#pragma unroll
+          for (int e = 0; e < HALF / 2; ++e) {
+            uint16_t lo, hi;
+            halves(vv.w[e], lo, hi);
+            fma_bf16(acc[2 * e], wb, lo);
+            fma_bf16(acc[2 * e + 1], wb, hi);
+          }
+        }
+        start_sums(tmem + ((uint32_t)rs << 16) + OUT0, acc);
+        if (lane < 16) {
+          stat[4 * ROWS + rs + lane] = fm;
+          stat[5 * ROWS + rs + lane] = fs;
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(far_over);
+        ok = wait_on(far_over, far_lap & 1u, abort_flag);
+        tc_fence_after();
+        if (half == 0) {
+          m = stat[4 * ROWS + r];
+          sum2 = pack2(stat[5 * ROWS + r], 0.f);
+        }
+      }
+      for (int j = 0; j < near && ok; ++j) {
+        const uint32_t n = base_t + (uint32_t)j;
+        const int k0 = key0 + j * TS + half * 32;            // this warp's keys: k0 .. k0 + 31
+        ok = wait_on(full + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
+        const uint32_t there = (uint32_t)(exist[n % STAGES] >> (32 * half));
+        ok = ok && wait_on(s_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t t_s = t_row + (n & 1u) * 64u + (uint32_t)half * 32u;
+        uint32_t w[16];
+        if (there && i_hi >= k0 && (T.dense || i_lo - (k0 + 31) <= P.l)) {      // some pair may be attended
+          uint32_t s[32];
+          tmem_ld32(t_s, s);
+          if (there != 0xffffffffu || T.dense || i_lo < k0 + 31 || i_hi - k0 > P.l) {   // some pair may not be
+            const int back0 = pos - k0;
+            if (T.dense) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((there >> e) & 1u) || !near_sees(T, pos, k0 + e)) s[e] = 0xFF800000u;   // -inf
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!((there >> e) & 1u) || (unsigned)(back0 - e) > (unsigned)P.l) s[e] = 0xFF800000u;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = fmaxf(mx[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * P.scale_log2;
+          const bool up = top > m + LAZY;                    // a first key (m = -inf) always moves the reference
+          if (__any_sync(0xffffffffu, up)) {
+            const float c = up ? ex2(m - top) : 1.f;         // 0 where nothing has been summed yet
+            const bool summed = up && m != -INFINITY;
+            if (up) m = top;
+            sum2 = mul2(sum2, pack2(c, c));
+            if (__any_sync(0xffffffffu, summed)) {           // this half's outputs so far, once the tile before has been added
+              ok = j == 0 || wait_on(o_done, (n - 1) & 1u, abort_flag);   // the first tile: sums of the strided keys
+              if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+              tc_fence_after();
+#pragma unroll 1
+              for (int g = 0; g < D_; g += 16) {
+                uint32_t v[16];
+                tmem_ld16_nowait(t_out + (uint32_t)g, v);
+                tmem_ld16_wait(v);
+                uint32_t lo[8], hi[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  lo[e] = __float_as_uint(__uint_as_float(v[e]) * c);
+                  hi[e] = __float_as_uint(__uint_as_float(v[e + 8]) * c);
+                }
+                tmem_st8(t_out + (uint32_t)g, lo);
+                tmem_st8(t_out + (uint32_t)(g + 8), hi);
+              }
+            }
+          }
+          const float nm = -mst_paged::reference(m);
+          const uint64_t nm2 = pack2(nm, nm);
+          uint64_t part[2] = {0ULL, 0ULL};
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t p = ex2_2(fma2(pack2(s[2 * e], s[2 * e + 1]), scale2, nm2));
+            part[e & 1] = add2(part[e & 1], p);
+            w[e] = pack_bf16_2(p);
+          }
+          sum2 = add2(sum2, add2(part[0], part[1]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = 0u;
+        }
+        tmem_st16(t_s, w);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8 * (n & 1u));
+      }
+      // the two softmaxes of a row meet: weights 2^(m_k - m), over the sum where the row is complete
+      float s_lo, s_hi;
+      unpack2(sum2, s_lo, s_hi);
+      stat[half * 2 * ROWS + r] = m;
+      stat[half * 2 * ROWS + ROWS + r] = s_lo + s_hi;
+      softmax_warps_meet();
+      const float ma = stat[r], mb = stat[2 * ROWS + r];
+      const float mm = fmaxf(ma, mb);
+      float a0 = ex2(ma - mst_paged::reference(mm)), a1 = ex2(mb - mst_paged::reference(mm));
+      const float total = fmaf(a0, stat[ROWS + r], a1 * stat[3 * ROWS + r]);
+      if (active == 1) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        a0 *= inv;
+        a1 *= inv;
+      }
+      ok = ok && wait_on(acc_full, lap & 1u, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      const int t = live ? (T.row0 + r) / P.group : 0, h = kvh * P.group + (live ? (T.row0 + r) % P.group : 0);
+      const int64_t token = T.first + t, at = ((int64_t)split * P.B.tokens + token) * P.heads + h;
+      bool bad = !(total * 0.f == 0.f);
+#pragma unroll
+      for (int pc = 0; pc < HALF / 16; ++pc) {
+        const int c = half * HALF + pc * 16;
+        uint32_t u[16], v[16];
+        tmem_ld16_nowait(t_row + OUT0 + (uint32_t)c, u);
+        tmem_ld16_nowait(t_row + OUT0 + D_ + (uint32_t)c, v);
+        tmem_ld16_wait(u);
+        tmem_ld16_wait(v);
+        float check = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float o = fmaf(a0, __uint_as_float(u[e]), a1 * __uint_as_float(v[e]));
+          check = fmaf(o, 0.f, check);
+          u[e] = __float_as_uint(o);
+        }
+        bad = bad || !(check == 0.f);
+        if (active == 1) {
+          stage_row(own + (uint32_t)(c / 64) * 2 * TILE_BYTES, r, c % 64, u, 1.f);
+        } else if (live && ok) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(P.part_o + at * D_ + c + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+        }
+      }
+      tc_fence_before();
+      if (live && ok && half == 0) {
+        if (active == 1) {
+          if (P.lse) P.lse[(int64_t)h * P.B.tokens + token] = (mm + log2f(total)) * LN2;
+        } else {
+          P.part_m[at * 2] = mm;
+          P.part_m[at * 2 + 1] = total;
+        }
+      }
+      const uint32_t redo = __ballot_sync(0xffffffffu, bad && live && ok);
+      if (lane == 0 && redo) atomicOr(&again[quarter], redo);
+      softmax_warps_meet();
+      if (active == 1 && ok) {
+#pragma unroll
+        for (int it = 0; it < 16; it += 4) {
+          const int rr = rs + it + (lane >> 3);
+          if (rr < T.rows) {
+            __nv_bfloat16* out = P.Out + (int64_t)(T.first + (T.row0 + rr) / P.group) * P.ldo + (int64_t)(kvh * P.group + (T.row0 + rr) % P.group) * D_ + (lane & 7) * 8;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<uint4*>(out + 64 * q) = lds128(piece_addr(own + q * 2 * TILE_BYTES, rr, lane & 7));
+          }
+        }
+      }
+      const bool any = (again[0] | again[1] | again[2] | again[3]) != 0u;
+      if (any) {       // seldom: rows that something masked and not finite reached
+        softmax_warps_meet();
+        for (int rr = warp; rr < T.rows; rr += CW) {
+          if (!((again[rr >> 5] >> (rr & 31)) & 1u)) continue;
+          float o[D_ / 32], gm, gs;
+          const int64_t to_key = (int64_t)key0 + (int64_t)near * TS;
+          row_again<D_>(P, T, b, kvh, rr, key0, have < to_key ? have : (int)to_key, P.l, m0, m1, o, gm, gs);
+          const int64_t tk = T.first + (T.row0 + rr) / P.group;
+          const int hh = kvh * P.group + (T.row0 + rr) % P.group;
+          if (active == 1) {
+            finish<D_ / 32>(P, tk, hh, lane, o, gm, gs);
+          } else {
+            const int64_t to = ((int64_t)split * P.B.tokens + tk) * P.heads + hh;
+#pragma unroll
+            for (int e = 0; e < D_ / 32; ++e) P.part_o[to * D_ + lane * (D_ / 32) + e] = o[e];
+            if (lane == 0) {
+              P.part_m[to * 2] = gm;
+              P.part_m[to * 2 + 1] = gs;
+            }
+          }
+        }
+        softmax_warps_meet();
+        if (warp == 0 && lane < ROWS / 32) again[lane] = 0u;
+      }
+      fence_async_smem();           // the own rows' place is written by the next tile's copy
+    }
+    if (__syncthreads_or(!ok || *abort_flag)) break;      // everybody is done with this tile of rows
+    ++lap;
+    if (m1 > m0) ++far_lap;
+    base_t += (uint32_t)near;
+  }
+  if (*abort_flag) {
+    for (int t = 0; t < 2000; ++t) __nanosleep(1000);   // let copies and products in flight land
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == CW + 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- maps and launch
+bool encode(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  mst_encode_tiled_fn fn = mst_encode_tiled();
+  if (!fn) return false;
+  const cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// rows of a box: the largest power of two up to 64 that divides a page
+int box_rows(int page_size) {
+  int r = 1;
+  while (r < TS && page_size % (2 * r) == 0) r *= 2;
+  return r;
+}
+// The cache as (values, then slots, heads and pages with the closest first); a dimension of one has whatever stride fits
+bool cache_maps(const Params& P, TileParams& A, CUtensorMap* tmK, CUtensorMap* tmV, int box) {
+  struct Dim { int what; int64_t n, stride; };
+  Dim d[3] = {{0, P.C.page_size, P.C.token_stride}, {1, P.C.kv_heads, P.C.head_stride}, {2, P.C.num_pages, P.C.page_stride}};
+  int64_t widest = P.C.D;
+  for (const Dim& x : d)
+    if (x.n > 1 && x.stride > widest) widest = x.stride;
+  for (Dim& x : d)
+    if (x.n <= 1) { x.n = 1; x.stride = widest; }
+  for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < 2; ++k)
+      if (d[k + 1].stride < d[k].stride) { const Dim t = d[k]; d[k] = d[k + 1]; d[k + 1] = t; }
+  cuuint64_t dims[4] = {(cuuint64_t)P.C.D, 1, 1, 1}, strides[3];
+  cuuint32_t boxes[4] = {64u, 1u, 1u, 1u};
+  for (int i = 0; i < 3; ++i) {
+    dims[i + 1] = (cuuint64_t)d[i].n;
+    strides[i] = (cuuint64_t)d[i].stride * 2;
+    if (strides[i] >= (1ULL << 40)) return false;
+    if (d[i].what == 0) { A.at_slot = i + 1; boxes[i + 1] = (cuuint32_t)box; }
+    if (d[i].what == 1) A.at_head = i + 1;
+    if (d[i].what == 2) A.at_page = i + 1;
+  }
+  return encode(tmK, P.C.K, 4, dims, strides, boxes) && encode(tmV, P.C.V, 4, dims, strides, boxes);
+}
+
+template <int D_>
+mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
+  MST_SMEM_LIMIT((paged_tiles_kernel<D_>), Shape<D_>::SMEM);
+  const dim3 grid((unsigned)(A.P.C.kv_heads * A.P.splits), (unsigned)A.P.B.batch, (unsigned)A.count);
+  MST_CUDA_TRY(mst_launch_overlapped(paged_tiles_kernel<D_>, grid, dim3(THREADS), Shape<D_>::SMEM, s, tmQ, tmK, tmV, A));
+  return MST_OK;
+}
+
+}  // namespace
+
+namespace mst_paged {
+mst_status_t launch_tiles(const Params& P, const Plan& plan, cudaStream_t s) {
+  TileParams A = {};
+  A.P = P;
+  A.rows = plan.rows;
+  A.count = plan.count;
+  CUtensorMap tmQ, tmK = {}, tmV = {};
+  const cuuint64_t dims[3] = {(cuuint64_t)P.C.D, (cuuint64_t)P.heads, (cuuint64_t)P.B.tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)P.C.D * 2, (cuuint64_t)P.ldq * 2};
+  const cuuint32_t boxes[3] = {64u, (cuuint32_t)P.group, (cuuint32_t)(plan.rows / P.group)};
+  if (strides[1] >= (1ULL << 40) || !encode(&tmQ, P.Q, 3, dims, strides, boxes)) return MST_ERR_SHAPE;
+  const int box = box_rows(P.C.page_size);
+  A.box = box >= 8 && P.C.num_pages > 0 && cache_maps(P, A, &tmK, &tmV, box) ? box : 0;
+  if (A.box == 0) tmK = tmV = tmQ;       // not read, but fetched ahead
+  return P.C.D == 64 ? launch<64>(A, tmQ, tmK, tmV, s) : launch<128>(A, tmQ, tmK, tmV, s);
+}
+}  // namespace mst_paged
+
+mst_status_t mst_paged_tiles_error_flags(int32_t* flags) {
+  int32_t bad = 0;
+  int v = 0;
+  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_page, &bad));
+  MST_CUDA_TRY(cudaMemcpyFromSymbol(&v, g_wait_error, sizeof(int)));
+  *flags = bad | (v << 1);
+  return MST_OK;
+}

@@ -42,6 +42,24 @@ int keys_of(int first, int end, int len, int tokens, int group, int stride, int6
   return 1;
 }
 
+// many rows: first, near, far; and the range's n0, n1, m0, m1, active
+int walk_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int splits, int least, int split,
+            int32_t* out) {
+  List T;
+  if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return -1;
+  const mst_paged::TileWalk w(T, reach);
+  int r[5] = {};
+  const int there = w.range(splits, least, split, r[0], r[1], r[2], r[3], r[4]);
+  out[0] = w.first; out[1] = w.near; out[2] = w.far;
+  for (int i = 0; i < 5; ++i) out[3 + i] = r[i];
+  return there;
+}
+int near(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int p, int k) {
+  List T;
+  if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return -1;
+  return mst_paged::near_sees(T, p, k);
+}
+
 int page(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int* slot) {
   return mst_paged::page_of(row, table_stride, page_size, num_pages, p, *slot);
 }

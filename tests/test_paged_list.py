@@ -74,6 +74,51 @@ def test_rows_look_at_their_sets(lib, n, length, group, R, stride):
         assert sorted(seen) == want and len(set(seen)) == len(seen)
 
 
+@pytest.mark.parametrize("stride", [(1 << 31) - 1, 64, 128, 100, 33, 7, 2])
+@pytest.mark.parametrize("n,length,group,R", [(1, 129, 40, 120), (7, 7, 3, 126), (40, 333, 1, 128), (9, 200, 40, 120), (130, 400, 1, 128),
+                                              (70, 500, 4, 128), (3, 2, 2, 128), (4, 0, 1, 128), (300, 700, 2, 128)])
+def test_tiles_of_many_rows_look_at_their_sets(lib, n, length, group, R, stride):
+    out, tile = (ctypes.c_int32 * 8)(), 0
+    rows = 0
+    while True:
+        args = _args(5, n, length, group, stride, BIG, tile, R)
+        info = _tile(lib, args)
+        if info is None:
+            break
+        row0, count, t_lo, nt, p_lo, p_hi, W, N, dense = info
+        positions = {p_lo + (row0 + r) // group - t_lo for r in range(count)}
+        seen = {p: [] for p in positions}
+        split, end, m_end = 0, 0, 2
+        while lib.walk_of(*args, 3, 2, split, out) == 1:
+            first, near, far, n0, n1, m0, m1, active = list(out)
+            assert n0 == end and m0 == m_end and m1 >= m0 and split < active <= 3 and (n1 > n0 or near == 0)
+            end, m_end = n1, m1
+            for p in positions:
+                seen[p] += [k for k in range(first + 64 * n0, first + 64 * n1) if lib.near(*args, p, k)]
+                seen[p] += [p - m * stride for m in range(m0, m1) if p - m * stride >= 0]
+            split += 1
+        assert end == near and m_end == 2 + far and split == active
+        for p in positions:
+            want = [j for j in range(p + 1) if p - j < stride or (p - j) % stride == 0]
+            assert sorted(seen[p]) == want
+        rows += count
+        tile += 1
+    assert rows == n * group
+
+
+@pytest.mark.parametrize("length", [-(1 << 31), -5, 0, (1 << 31) - 1, (1 << 30) + 7])
+@pytest.mark.parametrize("stride", [2, 64, 1000, (1 << 31) - 1])
+@pytest.mark.parametrize("reach", [0, 4096, BIG])
+def test_tiles_of_lengths_that_make_no_sense(lib, length, stride, reach):
+    out = (ctypes.c_int32 * 8)()
+    assert lib.walk_of(*_args(0, 300, length, 1, stride, reach, 1, 128), 16, 4, 0, out) == 1
+    first, near, far, n0, n1, m0, m1, active = list(out)
+    assert first >= 0 and first % 64 == 0 and 0 <= near <= 1 << 25 and far >= 0 and 1 <= active <= 16 and (near > 0) == (length > 300 - 128 - 128)
+    assert first + 64 * near <= max(length, 0) + 64
+    if reach < length:
+        assert near <= max(1, reach // 64 + 1)
+
+
 def test_rows_stay_within_the_table(lib):
     got = _seen_by_rows(lib, 4, 100, 1, 64, 16, 2, 1, 16, reach=80)
     for r, seen in got.items():
