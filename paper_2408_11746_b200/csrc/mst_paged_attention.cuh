@@ -68,15 +68,14 @@ __device__ __forceinline__ void finish(const Params& P, int64_t token, int h, in
 }
 
 // A row whose sums are not finite, formed again by one warp over the keys it looks at alone: what the matrix products multiplied by a weight
-// of zero may have been infinite or NaN.  Keys: positions from .. to - 1 as far as the row's window (distances up to `window`) has them, and the
-// strided ones m_from .. m_to - 1 steps back.  Lane: D / 32 neighbouring columns.
+// of zero may have been infinite or NaN.  The row of token row `row`, head h, position pos; keys: positions from .. to - 1 at distances up to
+// `window` (every: and at multiples of the stride), and the strided ones m_from .. m_to - 1 steps back.  Lane: D / 32 neighbouring columns.
 template <int D>
-static __device__ __noinline__ void row_again(const Params& P, const List T, int b, int kvh, int row, int from, int to, int window, int m_from, int m_to,
-                                       float (&o)[D / 32], float& m, float& sum) {
+static __device__ __noinline__ void row_again(const Params& P, int b, int row, int h, int pos, int from, int to, int window, bool every, int m_from,
+                                              int m_to, float (&o)[D / 32], float& m, float& sum) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31;
-  const int t = (T.row0 + row) / P.group, h = kvh * P.group + (T.row0 + row) % P.group, pos = T.p_lo + t - T.t_lo;
-  const __nv_bfloat16* q = P.Q + (int64_t)(T.first + t) * P.ldq + (int64_t)h * D + lane * E;
+  const __nv_bfloat16* q = P.Q + (int64_t)row * P.ldq + (int64_t)h * D + lane * E;
   m = -INFINITY;
   sum = 0.f;
 #pragma unroll
@@ -84,7 +83,7 @@ static __device__ __noinline__ void row_again(const Params& P, const List T, int
   auto add = [&](int j) {
     const Slot s = slot_of(P.C, P.B, b, j, &g_bad_page);
     if (!s.exists) return;
-    const int64_t at = s.at + (int64_t)kvh * P.C.head_stride + lane * E;
+    const int64_t at = s.at + (int64_t)(h / P.group) * P.C.head_stride + lane * E;
     float x = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) x = fmaf(__bfloat162float(q[e]), __bfloat162float(P.C.K[at + e]), x);
@@ -97,14 +96,13 @@ static __device__ __noinline__ void row_again(const Params& P, const List T, int
     for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, w * __bfloat162float(P.C.V[at + e]));
   };
   for (int j = from; j < to && j <= pos; ++j)
-    if (pos - j <= window || (T.dense && (pos - j) % T.l == 0)) add(j);
+    if (pos - j <= window || (every && (pos - j) % P.l == 0)) add(j);
   for (int k = m_from; k < m_to; ++k) {
-    const int64_t j = (int64_t)pos - (int64_t)k * T.l;
+    const int64_t j = (int64_t)pos - (int64_t)k * P.l;
     if (j < 0) break;
     add((int)j);
   }
 }
-
 
 struct Plan {
   bool tiles;             // 128-row tiles on the tensor cores, otherwise few rows

@@ -89,17 +89,18 @@ struct List {
 };
 
 // The same for tiles of many rows, whose keys come in tiles of 64 positions: near tiles first .. first + 64 near - 1 with every distance 0 .. l
-// (so the first strided key of every row too), then `far` steps: each row's key 2 l, 3 l, .. behind it, which no other row looks at.  A tile whose
-// last row has a position has one near tile at least.
+// (so the first strided key of every row too), then `far` steps: each row's key 2 l, 3 l, .. behind it, which no other row looks at.  Strides
+// below a tile (`dense`) have near tiles from 0 on and no steps.  A tile whose last row has a position has one near tile at least.
 constexpr int KEYS_OF_TILE = 64;
 struct TileWalk {
   int first, near, far;
   MST_HD TileWalk(const List& T, int64_t reach) {
-    const int64_t from = T.dense || (int64_t)T.p_lo - T.l < 0 ? 0 : (int64_t)T.p_lo - T.l;
+    const bool dense = T.l < KEYS_OF_TILE;
+    const int64_t from = dense || (int64_t)T.p_lo - T.l < 0 ? 0 : (int64_t)T.p_lo - T.l;
     const int64_t last = T.p_hi < reach ? T.p_hi : reach - 1;
     first = (int)(from / KEYS_OF_TILE) * KEYS_OF_TILE;
     near = T.p_hi < 0 ? 0 : last >= first ? (int)((last - first) / KEYS_OF_TILE) + 1 : 1;
-    far = T.dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - 1;
+    far = dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - 1;
   }
   // Range `split`: near tiles n0 .. n1 - 1, strided keys m0 .. m1 - 1 steps behind.  active: how many ranges there are, each with a near tile.
   MST_HD bool range(int splits, int least, int split, int& n0, int& n1, int& m0, int& m1, int& active) const {
@@ -115,9 +116,9 @@ struct TileWalk {
   }
 };
 // does a row at position p look at position k of a near tile
-MST_HD bool near_sees(const List& T, int p, int k) {
+MST_HD bool near_sees(int l, int p, int k) {
   const int back = p - k;
-  return back >= 0 && (back <= T.l || (T.dense && back % T.l == 0));
+  return back >= 0 && (back <= l || (l < KEYS_OF_TILE && back % l == 0));
 }
 
 // Page of position p >= 0 in a sequence's row of the table, -1 where there is none

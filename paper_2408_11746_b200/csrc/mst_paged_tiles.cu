@@ -104,7 +104,11 @@ __device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[64])
         : "memory");
 }
 
-template <int D_>
+// What a call's lists can have: nothing behind the window (NEAR: no position is two strides in), strided keys row by row (FAR), or the set in the
+// mask of every tile (DENSE: strides below a tile).  Code that is only jumped over costs registers here.
+enum Mode { NEAR, FAR, DENSE };
+
+template <int D_, Mode MODE>
 __global__ void __launch_bounds__(THREADS, Shape<D_>::BLOCKS)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                    const __grid_constant__ TileParams A) {
@@ -276,7 +280,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       if (lane == 0) {
         const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring, 16, 1024);
         const uint64_t step = S::STAGE_BYTES >> 4, part = TILE_BYTES >> 4;
-        const uint32_t from_far = m1 > m0 ? 1u : 0u;
+        const uint32_t from_far = MODE == FAR && m1 > m0 ? 1u : 0u;
         auto scores = [&](int j) {
           const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
           if (!wait_on(full + 8 * s, (n / STAGES) & 1u, abort_flag)) return false;
@@ -329,7 +333,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int i_lo = T.p_lo + (T.row0 + w0) / P.group - T.t_lo, i_hi = w0 < T.rows ? T.p_lo + (T.row0 + w1) / P.group - T.t_lo : -1;
       float m = -INFINITY;                                   // reference of this half's softmax, base 2
       uint64_t sum2 = 0ULL;
-      if (m1 > m0) {
+      if (MODE == FAR && m1 > m0) {
         const int fr = rs + (lane & 15);
         const bool there = fr < T.rows;
         const int fp = there ? T.p_lo + (T.row0 + fr) / P.group - T.t_lo : -1;
@@ -395,15 +399,15 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         tc_fence_after();
         const uint32_t t_s = t_row + (n & 1u) * 64u + (uint32_t)half * 32u;
         uint32_t w[16];
-        if (there && i_hi >= k0 && (T.dense || i_lo - (k0 + 31) <= P.l)) {      // some pair may be attended
+        if (there && i_hi >= k0 && (MODE == DENSE || i_lo - (k0 + 31) <= P.l)) {      // some pair may be attended
           uint32_t s[32];
           tmem_ld32(t_s, s);
-          if (there != 0xffffffffu || T.dense || i_lo < k0 + 31 || i_hi - k0 > P.l) {   // some pair may not be
+          if (MODE == DENSE || there != 0xffffffffu || i_lo < k0 + 31 || i_hi - k0 > P.l) {   // some pair may not be
             const int back0 = pos - k0;
-            if (T.dense) {
+            if (MODE == DENSE) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (!((there >> e) & 1u) || !near_sees(T, pos, k0 + e)) s[e] = 0xFF800000u;   // -inf
+                if (!((there >> e) & 1u) || !near_sees(P.l, pos, k0 + e)) s[e] = 0xFF800000u;   // -inf
             } else {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
@@ -480,7 +484,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       tc_fence_after();
       const int t = live ? (T.row0 + r) / P.group : 0, h = kvh * P.group + (live ? (T.row0 + r) % P.group : 0);
       const int64_t token = T.first + t, at = ((int64_t)split * P.B.tokens + token) * P.heads + h;
-      bool bad = !(total * 0.f == 0.f);
+      bool bad = !(total * 0.f == 0.f) || (MODE == NEAR && m1 > m0);     // (a length beyond what the table has room for: see launch)
 #pragma unroll
       for (int pc = 0; pc < HALF / 16; ++pc) {
         const int c = half * HALF + pc * 16;
@@ -534,9 +538,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           if (!((again[rr >> 5] >> (rr & 31)) & 1u)) continue;
           float o[D_ / 32], gm, gs;
           const int64_t to_key = (int64_t)key0 + (int64_t)near * TS;
-          row_again<D_>(P, T, b, kvh, rr, key0, have < to_key ? have : (int)to_key, P.l, m0, m1, o, gm, gs);
           const int64_t tk = T.first + (T.row0 + rr) / P.group;
           const int hh = kvh * P.group + (T.row0 + rr) % P.group;
+          row_again<D_>(P, b, (int)tk, hh, T.p_lo + (T.row0 + rr) / P.group - T.t_lo, key0, have < to_key ? have : (int)to_key, P.l, MODE == DENSE, m0, m1, o,
+                        gm, gs);
           if (active == 1) {
             finish<D_ / 32>(P, tk, hh, lane, o, gm, gs);
           } else {
@@ -556,7 +561,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     }
     if (__syncthreads_or(!ok || *abort_flag)) break;      // everybody is done with this tile of rows
     ++lap;
-    if (m1 > m0) ++far_lap;
+    if (MODE == FAR && m1 > m0) ++far_lap;
     base_t += (uint32_t)near;
   }
   if (*abort_flag) {
@@ -609,12 +614,19 @@ bool cache_maps(const Params& P, TileParams& A, CUtensorMap* tmK, CUtensorMap* t
   return encode(tmK, P.C.K, 4, dims, strides, boxes) && encode(tmV, P.C.V, 4, dims, strides, boxes);
 }
 
+template <int D_, Mode MODE>
+mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
+  MST_SMEM_LIMIT((paged_tiles_kernel<D_, MODE>), Shape<D_>::SMEM);
+  const dim3 grid((unsigned)(A.P.C.kv_heads * A.P.splits), (unsigned)A.P.B.batch, (unsigned)A.count);
+  MST_CUDA_TRY(mst_launch_overlapped(paged_tiles_kernel<D_, MODE>, grid, dim3(THREADS), Shape<D_>::SMEM, s, tmQ, tmK, tmV, A));
+  return MST_OK;
+}
 template <int D_>
 mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
-  MST_SMEM_LIMIT((paged_tiles_kernel<D_>), Shape<D_>::SMEM);
-  const dim3 grid((unsigned)(A.P.C.kv_heads * A.P.splits), (unsigned)A.P.B.batch, (unsigned)A.count);
-  MST_CUDA_TRY(mst_launch_overlapped(paged_tiles_kernel<D_>, grid, dim3(THREADS), Shape<D_>::SMEM, s, tmQ, tmK, tmV, A));
-  return MST_OK;
+  const int64_t reach = (int64_t)A.P.B.table_stride * A.P.C.page_size;
+  if (A.P.l < KEYS_OF_TILE) return launch<D_, DENSE>(A, tmQ, tmK, tmV, s);
+  // lengths beyond the table's room may still have rows two strides in, which are formed again key by key
+  return reach / 2 < A.P.l ? launch<D_, NEAR>(A, tmQ, tmK, tmV, s) : launch<D_, FAR>(A, tmQ, tmK, tmV, s);
 }
 
 }  // namespace

@@ -57,7 +57,7 @@ int walk_of(int first, int end, int len, int tokens, int group, int stride, int6
 int near(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int p, int k) {
   List T;
   if (!T.locate(first, end, len, tokens, group, stride, reach, tile, R)) return -1;
-  return mst_paged::near_sees(T, p, k);
+  return mst_paged::near_sees(T.l, p, k);
 }
 
 int page(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int* slot) {

@@ -148,13 +148,14 @@ def test_pages_that_do_not_exist(new, stride):
     assert mst.mst_device_error_flags() == 0
 
 
+@pytest.mark.parametrize("stride", [FAR, 64, 170])
 @pytest.mark.parametrize("new", [2, 90])
-def test_a_table_shorter_than_the_length(new):
+def test_a_table_shorter_than_the_length(new, stride):
     c = Case([new], [400], 2, 2, page=16)
     c.table = c.table[:, :20].contiguous()
     c.upload()
-    out, z = c.attend(FAR)
-    c.check(FAR, out, z, flags=BAD_PAGE)
+    out, z = c.attend(stride)
+    c.check(stride, out, z, flags=BAD_PAGE)
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
