@@ -55,6 +55,11 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
                "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0u;
+}
 __device__ __forceinline__ void softmax_warps_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // ---------------------------------------------------------------------------------------------- strided keys of a row
@@ -277,49 +282,57 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       ok = __all_sync(0xffffffffu, ok);
     } else if (warp == CW + 1) {
       // ------------------------------------------------------------------------------------------ products
-      if (lane == 0) {
-        const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring, 16, 1024);
-        const uint64_t step = S::STAGE_BYTES >> 4, part = TILE_BYTES >> 4;
-        const uint32_t from_far = MODE == FAR && m1 > m0 ? 1u : 0u;
-        auto scores = [&](int j) {
-          const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
-          if (!wait_on(full + 8 * s, (n / STAGES) & 1u, abort_flag)) return false;
-          tc_fence_after();
+      // The whole warp goes through the loop and one elected lane issues: what the instructions name is then worked out in uniform registers (by a
+      // lane of its own, issuing a tile's eleven instructions took 1300 clocks and was what the block waited for).
+      const bool leader = elect_one();
+      const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring, 16, 1024);
+      const uint64_t step = S::STAGE_BYTES >> 4, part = TILE_BYTES >> 4;
+      const uint32_t from_far = MODE == FAR && m1 > m0 ? 1u : 0u;
+      auto scores = [&](int j) {
+        const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
+        if (!__all_sync(0xffffffffu, wait_on(full + 8 * s, (n / STAGES) & 1u, abort_flag))) return false;
+        tc_fence_after();
+        if (leader) {
+          const uint64_t kd = kd0 + step * s;
+          const uint32_t d = tmem + (n & 1u) * 64u;
 #pragma unroll
           for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-              tc_mma(tmem + (n & 1u) * 64u, qd + 2 * part * q + 2 * ks, kd0 + step * s + part * q + 2 * ks, IDESC_K, (q > 0 || ks > 0) ? 1u : 0u);
+            for (int ks = 0; ks < 4; ++ks) tc_mma(d, qd + 2 * part * q + 2 * ks, kd + part * q + 2 * ks, IDESC_K, (q > 0 || ks > 0) ? 1u : 0u);
           tc_commit(s_full + 8 * (n & 1u));
-          return true;
-        };
-        ok = wait_on(own_full, lap & 1u, abort_flag);
-        ok = ok && scores(0);
-        if (ok && near > 1) ok = scores(1);
-        if (ok && from_far) {
-          ok = wait_on(far_over, far_lap & 1u, abort_flag);
-          tc_fence_after();
         }
-        for (int j = 0; j < near && ok; ++j) {
-          const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
-          ok = wait_on(p_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
+        __syncwarp();
+        return true;
+      };
+      ok = __all_sync(0xffffffffu, wait_on(own_full, lap & 1u, abort_flag));
+      ok = ok && scores(0);
+      if (ok && near > 1) ok = scores(1);
+      if (ok && from_far) {
+        ok = __all_sync(0xffffffffu, wait_on(far_over, far_lap & 1u, abort_flag));
+        tc_fence_after();
+      }
+      for (int j = 0; j < near && ok; ++j) {
+        const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
+        ok = __all_sync(0xffffffffu, wait_on(p_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        if (leader) {
           const uint32_t p = tmem + (n & 1u) * 64u;
           const uint64_t vd = kd0 + step * s + part * PARTS;
+          const uint32_t more = j > 0 ? 1u : 0u;
 #pragma unroll
           for (int q = 0; q < PARTS; ++q)
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)   // 16 keys each: two of the first half's 32, two of the second's
               tc_mma_ts(tmem + OUT0 + (uint32_t)((ks >> 1) * D_ + 64 * q), p + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8),
-                        vd + part * q + (uint64_t)(ks * ((16 * 128) >> 4)), IDESC_MN, (j > 0 || (ks & 1)) ? 1u : ks == 0 ? from_far : 0u);
+                        vd + part * q + (uint64_t)(ks * ((16 * 128) >> 4)), IDESC_MN, (ks & 1) ? 1u : ks == 0 ? more | from_far : more);
           tc_commit(empty + 8 * s);
           tc_commit(o_done);
           if (j + 1 == near) tc_commit(acc_full);
-          if (j + 2 < near) ok = scores(j + 2);
         }
+        __syncwarp();
+        if (j + 2 < near) ok = scores(j + 2);
       }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
     } else {
       // ------------------------------------------------------------------------------------------ softmax
       const int quarter = warp & 3, half = warp >> 2;
