@@ -331,12 +331,12 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + p.rows - 1) / p.rows, most = p.tiles ? 65535 : 65535 / c.kv_heads;
   p.count = (int)(tiles < most ? tiles : most);
-  // units of the longest list: 64 entries, or tiles of 64 keys
+  // units of the longest list: 64 entries, or tiles of 128 keys
   const int64_t nt = (p.rows + group - 1) / group;
   int64_t units;
   if (p.tiles) {
-    units = (stride >= len ? len : stride + nt < len ? stride + nt : len) / UNIT + 1;
-    p.least = 16;
+    units = (stride >= len || stride < DENSE_BELOW ? len : stride + nt < len ? stride + nt : len) / KEYS_OF_TILE + 1;
+    p.least = 8;
   } else {
     const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
     units = (list + UNIT - 1) / UNIT;

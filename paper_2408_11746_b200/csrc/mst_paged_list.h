@@ -88,14 +88,15 @@ struct List {
   }
 };
 
-// The same for tiles of many rows, whose keys come in tiles of 64 positions: near tiles first .. first + 64 near - 1 with every distance 0 .. l
-// (so the first strided key of every row too), then `far` steps: each row's key 2 l, 3 l, .. behind it, which no other row looks at.  Strides
-// below a tile (`dense`) have near tiles from 0 on and no steps.  A tile whose last row has a position has one near tile at least.
-constexpr int KEYS_OF_TILE = 64;
+// The same for tiles of many rows, whose keys come in tiles of 128 positions: `near` of them from `first` on with every distance 0 .. l (so the
+// first strided key of every row too), then `far` steps: each row's key 2 l, 3 l, .. behind it, which no other row looks at.  Short strides
+// (`dense`: 64 keys in a tile take about as long as one step) have near tiles from 0 on and no steps.  A tile whose last row has a position has one near
+// tile at least.
+constexpr int KEYS_OF_TILE = 128, DENSE_BELOW = 64;
 struct TileWalk {
   int first, near, far;
   MST_HD TileWalk(const List& T, int64_t reach) {
-    const bool dense = T.l < KEYS_OF_TILE;
+    const bool dense = T.l < DENSE_BELOW;
     const int64_t from = dense || (int64_t)T.p_lo - T.l < 0 ? 0 : (int64_t)T.p_lo - T.l;
     const int64_t last = T.p_hi < reach ? T.p_hi : reach - 1;
     first = (int)(from / KEYS_OF_TILE) * KEYS_OF_TILE;
@@ -118,7 +119,7 @@ struct TileWalk {
 // does a row at position p look at position k of a near tile
 MST_HD bool near_sees(int l, int p, int k) {
   const int back = p - k;
-  return back >= 0 && (back <= l || (l < KEYS_OF_TILE && back % l == 0));
+  return back >= 0 && (back <= l || (l < DENSE_BELOW && back % l == 0));
 }
 
 // Page of position p >= 0 in a sequence's row of the table, -1 where there is none

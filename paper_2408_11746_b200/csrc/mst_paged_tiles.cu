@@ -1,16 +1,20 @@
 // Attention over a paged cache for many rows (chunks of prompts): tiles of up to 128 (token, head) rows of one key head on the tensor cores.
-// Keys come in tiles of 64 positions (mst_paged_list.h: TileWalk); the strided keys further back, which one row each looks at, are formed row by
+// Keys come in tiles of 128 positions (mst_paged_list.h: TileWalk); the strided keys further back, which one row each looks at, are formed row by
 // row and are where the first half's softmax starts.  Roles of a block's ten warps:
-//   warps 0-7  softmax: thread = row (tensor-memory lane), the two warps of a lane quarter take 32 of a tile's 64 keys each, as softmaxes of
-//              their own - reference, sum and output accumulator - that meet when the rows leave;
-//   warp 8     fills a four-slot ring: pages whose positions fall on whole boxes by TMA, one box a page and tile at most 64 rows high; the tile
+//   warps 0-7  softmax: thread = row (tensor-memory lane), the two warps of a lane quarter take 64 of a tile's 128 keys each.  The halves are
+//              pipelines of their own - scores, weights, reference, sum, output accumulator - that share the loads only and meet when the rows
+//              leave: one's products are under way while the other takes exponentials;
+//   warp 8     fills rings of two key and two value tiles: pages whose positions fall on whole boxes by TMA, a box at most 64 rows high; the tile
 //              in which a sequence ends, pages that do not exist and page sizes without a factor of eight by 16-byte asynchronous copies, zeros
-//              where nothing is (what a page holds behind the length may be no number).  Which of a tile's keys exist goes with the slot;
-//   warp 9     one lane issues tcgen05.mma: S = Q K^T (128 x 64) two tiles ahead, O_half += P V over the half's 32 keys, P read from tensor
-//              memory where the softmax warps have written it over the scores.
-// Tensor memory: scores in columns 0-63 and 64-127, the halves' outputs behind.  Ranges of a list (blockIdx.x) leave sums for the join.
-// Bound: exponentials (16 a clock and SM: 512 clocks a 128 x 64 tile, the products need 256), two blocks an SM at head_dim 64.
+//              where nothing is (what a page holds behind the length may be no number);
+//   warp 9     tcgen05.mma: S_half = Q K_half^T (128 x 64), O_half += P_half V_half, P read from tensor memory where the softmax warps have
+//              written it over the scores.
+// Tensor memory: the halves' scores in columns 0-63 and 64-127, their outputs behind: two blocks an SM at head_dim 64.  Ranges of a list (blockIdx.x)
+// leave sums for the join.
+// Bound: exponentials (16 a clock and SM: 1024 clocks for 128 x 128, the products need 640).
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "mst_paged_attention.cuh"
 
@@ -21,17 +25,17 @@ using mst_ptx::pack_bf16;
 
 __device__ int g_wait_error = 0;
 
-constexpr int STAGES = 4;
-constexpr int LAG = 2;            // tiles of plain copies under way before the oldest is waited for
+constexpr int STAGES = 2;
+constexpr int KEYS = KEYS_OF_TILE;
 template <int D_>
 struct Shape {
   static constexpr int PARTS = D_ / 64;                            // 64 columns each: 128 bytes a row
   static constexpr int OWN_BYTES = PARTS * 2 * TILE_BYTES;
-  static constexpr int STAGE_BYTES = PARTS * 2 * TILE_BYTES;       // keys, then values
+  static constexpr int SLOT_BYTES = PARTS * 2 * TILE_BYTES;        // 128 keys, or their values
   static constexpr int TMEM_COLS = D_ == 64 ? 256 : 512;
   static constexpr int BLOCKS = D_ == 64 ? 2 : 1;
-  // own rows, ring, statistics, which keys exist, barriers (full, empty, own_full, s_full[2], p_full[2], o_done, acc_full, far_over)
-  static constexpr int SMEM = OWN_BYTES + STAGES * STAGE_BYTES + 3 * 2 * ROWS * 4 + STAGES * 8 + 16 * STAGES + 8 * 8 + 1024;
+  // own rows, rings, statistics, which keys exist, barriers (full and empty of both rings, own_full, s_full[2], p_full[2], acc_full, far_over)
+  static constexpr int SMEM = OWN_BYTES + STAGES * 2 * SLOT_BYTES + 3 * 2 * ROWS * 4 + STAGES * 16 + 32 * STAGES + 7 * 8 + 1024;
 };
 
 struct TileParams {
@@ -42,8 +46,31 @@ struct TileParams {
   int at_slot, at_head, at_page;   // which of the map's coordinates 1 .. 3 they are
 };
 
+// mbar_wait, but asleep in the barrier for up to 2 us at a time: the warps that wait here share their schedulers with those that count
 __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return mbar_wait(bar, parity, abort_flag, &g_wait_error);
+  for (uint32_t it = 0;; ++it) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(2000u)
+        : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+    if (it > MST_SPIN_LIMIT / 4) {
+      *abort_flag = 1;
+      atomicOr(&g_wait_error, 1);
+      return false;
+    }
+  }
+}
+constexpr float MOST = 65536.f;
+__device__ __forceinline__ float halves_sum(uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
 }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(tm),
@@ -55,10 +82,31 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
                "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ bool elect_one() {
+__device__ __forceinline__ uint32_t elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(one));
-  return one != 0u;
+  return one;
+}
+// The instructions of a whole warp of which the elected lane's counts: no branch around them, so that what they name stays uniform
+__device__ __forceinline__ void mma_ss(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(IDESC_K), "r"(accum), "r"(one)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t one, uint32_t d, uint32_t a, uint64_t b, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(IDESC_MN), "r"(accum), "r"(one)
+      : "memory");
+}
+__device__ __forceinline__ void commit_to(uint32_t one, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(one)
+      : "memory");
 }
 __device__ __forceinline__ void softmax_warps_meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
@@ -110,7 +158,7 @@ __device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[64])
 }
 
 // What a call's lists can have: nothing behind the window (NEAR: no position is two strides in), strided keys row by row (FAR), or the set in the
-// mask of every tile (DENSE: strides below a tile).  Code that is only jumped over costs registers here.
+// mask of every tile (DENSE: short strides).  Code that is only jumped over costs registers here.
 enum Mode { NEAR, FAR, DENSE };
 
 template <int D_, Mode MODE>
@@ -121,11 +169,13 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   constexpr int PARTS = S::PARTS, HALF = D_ / 2, OUT0 = 128;     // OUT0: tensor-memory column of the first half's outputs
   const Params& P = A.P;
   extern __shared__ unsigned char smem_raw[];
-  const uint32_t own = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = own + S::OWN_BYTES, stat_a = ring + STAGES * S::STAGE_BYTES;
-  const uint32_t exist_a = stat_a + 3 * 2 * ROWS * 4, full = exist_a + 8 * STAGES, empty = full + 8 * STAGES, own_full = empty + 8 * STAGES,
-                 s_full = own_full + 8, p_full = s_full + 16, o_done = p_full + 16, acc_full = o_done + 8, far_over = acc_full + 8;
+  const uint32_t own = (smem_u32(smem_raw) + 1023u) & ~1023u, ring_k = own + S::OWN_BYTES, ring_v = ring_k + STAGES * S::SLOT_BYTES,
+                 stat_a = ring_v + STAGES * S::SLOT_BYTES;
+  const uint32_t exist_a = stat_a + 3 * 2 * ROWS * 4, full_k = exist_a + 16 * STAGES, full_v = full_k + 8 * STAGES, empty_k = full_v + 8 * STAGES,
+                 empty_v = empty_k + 8 * STAGES, own_full = empty_v + 8 * STAGES, s_full = own_full + 8, p_full = s_full + 16, acc_full = p_full + 16,
+                 far_over = acc_full + 8;
   unsigned char* base = smem_raw + (own - smem_u32(smem_raw));
-  volatile unsigned long long* exist = reinterpret_cast<unsigned long long*>(base + (exist_a - own));
+  volatile uint32_t* exist = reinterpret_cast<uint32_t*>(base + (exist_a - own));     // [STAGES][4]
   __shared__ uint32_t holder;
   __shared__ uint32_t again[ROWS / 32];
   __shared__ int abort_sh;
@@ -133,16 +183,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     abort_sh = 0;
-    for (int s = 0; s < STAGES; ++s) {
-      mbar_init(full + 8 * s, 1);
-      mbar_init(empty + 8 * s, 1);
-    }
+    for (int s = 0; s < 4 * STAGES; ++s) mbar_init(full_k + 8 * s, 1);
     mbar_init(own_full, 1);
-    for (int e = 0; e < 2; ++e) {
-      mbar_init(s_full + 8 * e, 1);
-      mbar_init(p_full + 8 * e, CW);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(s_full + 8 * h, 1);
+      mbar_init(p_full + 8 * h, CW / 2);
     }
-    mbar_init(o_done, 1);
     mbar_init(acc_full, 1);
     mbar_init(far_over, CW);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -167,15 +213,14 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   const int64_t all = P.B.first[b + 1] > P.B.first[b] ? ((int64_t)P.B.first[b + 1] - P.B.first[b]) * P.group : 0;
   const int tiles = (int)((all + A.rows - 1) / A.rows);
   uint32_t lap = 0, far_lap = 0;   // tiles of rows so far, those with strided keys: barriers that complete once in each
-  uint32_t base_t = 0;  // near tiles so far: ring places and score buffers go on from tile to tile
-  bool ok = true;
+  uint32_t base_t = 0;  // near tiles so far: ring places go on from tile to tile
   for (int z = (int)blockIdx.z; z < tiles; z += A.count) {
     List T;
     if (!locate(T, P, b, tiles - 1 - z, A.rows)) break;
     const TileWalk walk(T, reach);
     int n0, n1, m0, m1, active;
     if (!walk.range(P.splits, P.least, split, n0, n1, m0, m1, active)) continue;
-    const int near = n1 - n0, key0 = walk.first + n0 * TS;
+    const int near = n1 - n0, key0 = walk.first + n0 * KEYS;
     if (near == 0) {      // no row has a position
       if (warp < CW)
         for (int r = warp; r < T.rows; r += CW) {
@@ -184,6 +229,19 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
       continue;
     }
+    // do all the range's pages exist (keys behind a sequence's end are behind every row of it)
+    const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
+    bool hole = len > reach;
+    {
+      const int64_t end = (int64_t)key0 + (int64_t)near * KEYS;
+      const int p1 = have > 0 ? ((int)(end < have ? end : have) - 1) / P.C.page_size : -1;
+      for (int p = key0 / P.C.page_size + (int)threadIdx.x; p <= p1; p += THREADS) {
+        const int id = table[p];
+        hole = hole || id < 0 || id >= P.C.num_pages;
+      }
+    }
+    hole = __syncthreads_or(hole) != 0;
+    // A wait that gives up sets the block's abort flag, after which every wait returns at once: nobody leaves his loop early, and nothing is stored
     if (warp == CW) {
       // ------------------------------------------------------------------------------------------ loads
       if (lane == 0) {
@@ -192,146 +250,163 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         for (int c = 0; c < PARTS; ++c)
           tma_load_3d(own + c * 2 * TILE_BYTES, &tmQ, 64 * c, kvh * P.group, T.first + T.t_lo, own_full);
       }
-      int waiting = 0;       // tiles of plain copies whose slots have not been given out
-      uint32_t oldest = 0;
-      auto give = [&]() {
+      bool waiting = false;  // plain copies of the tile before are under way
+      auto give = [&](uint32_t n) {
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(full + 8 * (oldest % STAGES));
-        ++oldest;
-        --waiting;
+        if (lane == 0) {
+          mbar_arrive(full_k + 8 * (n % STAGES));
+          mbar_arrive(full_v + 8 * (n % STAGES));
+        }
+        waiting = false;
       };
-      const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
-      for (int j = 0; j < near && ok; ++j) {
+      for (int j = 0; j < near; ++j) {
         const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
-        const int k0 = key0 + j * TS;
-        const uint32_t dst = ring + s * S::STAGE_BYTES, bar = full + 8 * s;
-        bool whole = A.box > 0 && k0 + TS <= have;
+        const int k0 = key0 + j * KEYS;
+        const uint32_t to_k = ring_k + s * S::SLOT_BYTES, to_v = ring_v + s * S::SLOT_BYTES;
+        bool whole = A.box > 0 && KEYS <= have - k0;
         int id = 0, slot = 0;
-        const bool mine = whole && lane * A.box < TS;
+        const bool mine = whole && lane * A.box < KEYS;
         if (mine) id = page_of(table, P.B.table_stride, P.C.page_size, P.C.num_pages, k0 + lane * A.box, slot);
         whole = whole && __all_sync(0xffffffffu, id >= 0);
-        if (whole)
-          while (waiting > 0) {
-            cp_wait<0>();
-            give();
-          }
-        if (n >= STAGES) ok = wait_on(empty + 8 * s, (n / STAGES - 1) & 1u, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        const uint32_t before = (n / STAGES - 1) & 1u;
+        if (waiting) {        // ahead of any wait for a slot: the products of the tile before that one may be waiting for these keys
+          cp_wait<0>();
+          give(n - 1);
+        }
         if (whole) {
-          if (lane == 0) {
-            exist[s] = ~0ULL;
-            mbar_expect_tx(bar, S::STAGE_BYTES);
+          int c[4];
+#pragma unroll
+          for (int d = 1; d < 4; ++d) c[d] = d == A.at_slot ? slot : d == A.at_head ? kvh : id;
+          if (n >= STAGES) wait_on(empty_k + 8 * s, before, abort_flag);
+          __syncwarp();
+          if (lane == 0) mbar_expect_tx(full_k + 8 * s, S::SLOT_BYTES);
+          __syncwarp();
+          if (mine)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q)
+              tma_load_4d(to_k + (uint32_t)(q * 2 * TILE_BYTES + lane * A.box * 128), &tmK, 64 * q, c[1], c[2], c[3], full_k + 8 * s);
+          if (n >= STAGES) wait_on(empty_v + 8 * s, before, abort_flag);     // then nobody reads `exist` of the tile before either
+          __syncwarp();
+          if (lane < 4 && hole) exist[4 * s + lane] = ~0u;
+          __syncwarp();
+          if (lane == 0) mbar_expect_tx(full_v + 8 * s, S::SLOT_BYTES);
+          __syncwarp();
+          if (mine)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q)
+              tma_load_4d(to_v + (uint32_t)(q * 2 * TILE_BYTES + lane * A.box * 128), &tmV, 64 * q, c[1], c[2], c[3], full_v + 8 * s);
+        } else {
+          if (n >= STAGES) {
+            wait_on(empty_k + 8 * s, before, abort_flag);
+            wait_on(empty_v + 8 * s, before, abort_flag);
           }
           __syncwarp();
-          if (mine) {
-            int c[4];
-#pragma unroll
-            for (int d = 1; d < 4; ++d) c[d] = d == A.at_slot ? slot : d == A.at_head ? kvh : id;
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) {
-              const uint32_t to = dst + (uint32_t)(q * TILE_BYTES + lane * A.box * 128);
-              tma_load_4d(to, &tmK, 64 * q, c[1], c[2], c[3], bar);
-              tma_load_4d(to + PARTS * TILE_BYTES, &tmV, 64 * q, c[1], c[2], c[3], bar);
-            }
-          }
-        } else {
-          if (waiting == 0) oldest = n;
-          int64_t at[2];
-          bool there[2];
-          unsigned long long bits = 0ULL;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int k = k0 + 32 * u + lane;
-            at[u] = 0;
-            there[u] = false;
-            if (k < have) {
-              const Slot sl = slot_of(P.C, P.B, b, k, &g_bad_page);
-              there[u] = sl.exists;
-              if (sl.exists) at[u] = sl.at + (int64_t)kvh * P.C.head_stride;
-            }
-            bits |= (unsigned long long)__ballot_sync(0xffffffffu, there[u]) << (32 * u);
-          }
-          if (lane == 0) exist[s] = bits;
           constexpr int PIECES = D_ / 8, AT_ONCE = 32 / PIECES;
           const int c = lane % PIECES;
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
+#pragma unroll 1
+          for (int u = 0; u < KEYS / 32; ++u) {
+            const int k = k0 + 32 * u + lane;
+            int64_t at = 0;
+            bool there = false;
+            if (k < have) {
+              const Slot sl = slot_of(P.C, P.B, b, k, &g_bad_page);
+              there = sl.exists;
+              if (sl.exists) at = sl.at + (int64_t)kvh * P.C.head_stride;
+            }
+            const uint32_t bits = __ballot_sync(0xffffffffu, there);
+            if (lane == 0) exist[4 * s + u] = bits;
 #pragma unroll 4
             for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
               const int r = r0 + lane / PIECES;
-              const int64_t a = __shfl_sync(0xffffffffu, at[u], r);
-              const bool in = __shfl_sync(0xffffffffu, there[u], r);
-              const uint32_t to = piece_addr(dst + (uint32_t)(c / 8) * TILE_BYTES, 32 * u + r, c % 8);
-              cp16(to, P.C.K + a + c * 8, in);
-              cp16(to + PARTS * TILE_BYTES, P.C.V + a + c * 8, in);
+              const int64_t a = __shfl_sync(0xffffffffu, at, r);
+              const bool in = (bits >> r) & 1u;
+              const uint32_t to = piece_addr((uint32_t)(c / 8) * 2 * TILE_BYTES, 32 * u + r, c % 8);
+              cp16(to_k + to, P.C.K + a + c * 8, in);
+              cp16(to_v + to, P.C.V + a + c * 8, in);
             }
-          cp_commit();
-          ++waiting;
-          if (waiting > LAG) {
-            cp_wait<LAG>();
-            give();
           }
+          cp_commit();
+          waiting = true;
         }
       }
-      while (waiting > 0 && ok) {
+      if (waiting) {
         cp_wait<0>();
-        give();
+        give(base_t + (uint32_t)near - 1);
       }
-      cp_wait<0>();
-      ok = __all_sync(0xffffffffu, ok);
     } else if (warp == CW + 1) {
       // ------------------------------------------------------------------------------------------ products
-      // The whole warp goes through the loop and one elected lane issues: what the instructions name is then worked out in uniform registers (by a
-      // lane of its own, issuing a tile's eleven instructions took 1300 clocks and was what the block waited for).
-      const bool leader = elect_one();
-      const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring, 16, 1024);
-      const uint64_t step = S::STAGE_BYTES >> 4, part = TILE_BYTES >> 4;
+      // The whole warp goes through the loop and one elected lane issues.  What the instructions name is the same in every turn, a slot's and a half's
+      // part being constants, and stays in uniform registers (by a lane of its own, with addresses worked out on the way, a tile's instructions took
+      // 1300 clocks to issue).
+      const uint32_t leader = elect_one();
+      const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring_k, 16, 1024), vd0 = smem_desc(ring_v, 16, 1024);
+      constexpr uint64_t step = S::SLOT_BYTES >> 4, part = (2 * TILE_BYTES) >> 4, half_tile = TILE_BYTES >> 4;
       const uint32_t from_far = MODE == FAR && m1 > m0 ? 1u : 0u;
-      auto scores = [&](int j) {
-        const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
-        if (!__all_sync(0xffffffffu, wait_on(full + 8 * s, (n / STAGES) & 1u, abort_flag))) return false;
-        tc_fence_after();
-        if (leader) {
-          const uint64_t kd = kd0 + step * s;
-          const uint32_t d = tmem + (n & 1u) * 64u;
+      auto scores = [&](auto slot, auto half) {
+        constexpr uint32_t SL = decltype(slot)::value, H = decltype(half)::value;
 #pragma unroll
-          for (int q = 0; q < PARTS; ++q)
+        for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) tc_mma(d, qd + 2 * part * q + 2 * ks, kd + part * q + 2 * ks, IDESC_K, (q > 0 || ks > 0) ? 1u : 0u);
-          tc_commit(s_full + 8 * (n & 1u));
-        }
+          for (int ks = 0; ks < 4; ++ks)
+            mma_ss(leader, tmem + H * 64u, qd + part * q + 2 * ks, kd0 + step * SL + part * q + half_tile * H + 2 * ks, (q > 0 || ks > 0) ? 1u : 0u);
+        commit_to(leader, s_full + 8 * H);
+        if (H == 1) commit_to(leader, empty_k + 8 * SL);
         __syncwarp();
-        return true;
       };
-      ok = __all_sync(0xffffffffu, wait_on(own_full, lap & 1u, abort_flag));
-      ok = ok && scores(0);
-      if (ok && near > 1) ok = scores(1);
-      if (ok && from_far) {
-        ok = __all_sync(0xffffffffu, wait_on(far_over, far_lap & 1u, abort_flag));
-        tc_fence_after();
-      }
-      for (int j = 0; j < near && ok; ++j) {
-        const uint32_t n = base_t + (uint32_t)j, s = n % STAGES;
-        ok = __all_sync(0xffffffffu, wait_on(p_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag));
-        if (!ok) break;
-        tc_fence_after();
-        if (leader) {
-          const uint32_t p = tmem + (n & 1u) * 64u;
-          const uint64_t vd = kd0 + step * s + part * PARTS;
-          const uint32_t more = j > 0 ? 1u : 0u;
+      auto outputs = [&](auto slot, auto half, uint32_t more, bool last) {
+        constexpr uint32_t SL = decltype(slot)::value, H = decltype(half)::value;
 #pragma unroll
-          for (int q = 0; q < PARTS; ++q)
+        for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)   // 16 keys each: two of the first half's 32, two of the second's
-              tc_mma_ts(tmem + OUT0 + (uint32_t)((ks >> 1) * D_ + 64 * q), p + (uint32_t)((ks >> 1) * 32 + (ks & 1) * 8),
-                        vd + part * q + (uint64_t)(ks * ((16 * 128) >> 4)), IDESC_MN, (ks & 1) ? 1u : ks == 0 ? more | from_far : more);
-          tc_commit(empty + 8 * s);
-          tc_commit(o_done);
-          if (j + 1 == near) tc_commit(acc_full);
+          for (int ks = 0; ks < 4; ++ks)
+            mma_ts(leader, tmem + OUT0 + (uint32_t)(H * D_ + 64 * q), tmem + (uint32_t)(H * 64 + ks * 8),
+                   vd0 + step * SL + part * q + half_tile * H + (uint64_t)(ks * ((16 * 128) >> 4)), ks ? 1u : more);
+        if (H == 1) {
+          commit_to(leader, empty_v + 8 * SL);
+          if (last) commit_to(leader, acc_full);
         }
         __syncwarp();
-        if (j + 2 < near) ok = scores(j + 2);
+      };
+      constexpr std::integral_constant<uint32_t, 0> C0{};
+      constexpr std::integral_constant<uint32_t, 1> C1{};
+      auto keys_in = [&](uint32_t n) {
+        wait_on(full_k + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+      };
+      // tile j in slot `here`: its weights are used up half by half, the next tile's scores follow in the other slot
+      auto turn = [&](int j, auto here, auto there) {
+        const uint32_t n = base_t + (uint32_t)j;
+        const bool last = j + 1 == near;
+        wait_on(full_v + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
+        wait_on(p_full, n & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        outputs(here, C0, (j > 0 ? 1u : 0u) | from_far, last);
+        if (!last) {
+          keys_in(n + 1);
+          scores(there, C0);
+        }
+        wait_on(p_full + 8, n & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        outputs(here, C1, j > 0 ? 1u : 0u, last);
+        if (!last) scores(there, C1);
+      };
+      static_assert(STAGES == 2, "slots take turns");
+      wait_on(own_full, lap & 1u, abort_flag);
+      keys_in(base_t);
+      if (base_t % 2 == 0) {
+        scores(C0, C0);
+        scores(C0, C1);
+      } else {
+        scores(C1, C0);
+        scores(C1, C1);
+      }
+      for (int j = 0; j < near; ++j) {
+        if ((base_t + (uint32_t)j) % 2 == 0) turn(j, C0, C1);
+        else turn(j, C1, C0);
       }
     } else {
       // ------------------------------------------------------------------------------------------ softmax
@@ -345,7 +420,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int w0 = quarter * 32, w1 = w0 + 31 < T.rows ? w0 + 31 : T.rows - 1;     // this warp's rows
       const int i_lo = T.p_lo + (T.row0 + w0) / P.group - T.t_lo, i_hi = w0 < T.rows ? T.p_lo + (T.row0 + w1) / P.group - T.t_lo : -1;
       float m = -INFINITY;                                   // reference of this half's softmax, base 2
-      uint64_t sum2 = 0ULL;
+      float total_w = 0.f;
       if (MODE == FAR && m1 > m0) {
         const int fr = rs + (lane & 15);
         const bool there = fr < T.rows;
@@ -395,93 +470,105 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(far_over);
-        ok = wait_on(far_over, far_lap & 1u, abort_flag);
+        wait_on(far_over, far_lap & 1u, abort_flag);
+        __syncwarp();
         tc_fence_after();
         if (half == 0) {
           m = stat[4 * ROWS + r];
-          sum2 = pack2(stat[5 * ROWS + r], 0.f);
+          total_w = stat[5 * ROWS + r];
         }
       }
-      for (int j = 0; j < near && ok; ++j) {
+      for (int j = 0; j < near; ++j) {
         const uint32_t n = base_t + (uint32_t)j;
-        const int k0 = key0 + j * TS + half * 32;            // this warp's keys: k0 .. k0 + 31
-        ok = wait_on(full + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
-        const uint32_t there = (uint32_t)(exist[n % STAGES] >> (32 * half));
-        ok = ok && wait_on(s_full + 8 * (n & 1u), (n >> 1) & 1u, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (hole) wait_on(full_v + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);       // with it `exist`
+        wait_on(s_full + 8 * half, n & 1u, abort_flag);
+        __syncwarp();
         tc_fence_after();
-        const uint32_t t_s = t_row + (n & 1u) * 64u + (uint32_t)half * 32u;
-        uint32_t w[16];
-        if (there && i_hi >= k0 && (MODE == DENSE || i_lo - (k0 + 31) <= P.l)) {      // some pair may be attended
-          uint32_t s[32];
-          tmem_ld32(t_s, s);
-          if (MODE == DENSE || there != 0xffffffffu || i_lo < k0 + 31 || i_hi - k0 > P.l) {   // some pair may not be
-            const int back0 = pos - k0;
-            if (MODE == DENSE) {
+        const int k0 = key0 + j * KEYS + half * 64;            // this warp's keys: k0 .. k0 + 63
+        uint32_t there[2] = {~0u, ~0u};
+        if (hole) {
+          there[0] = exist[4 * (n % STAGES) + 2 * half];
+          there[1] = exist[4 * (n % STAGES) + 2 * half + 1];
+        }
+        const uint32_t t_s = t_row + (uint32_t)(half * 64);
+        uint32_t w[32];
+        if ((there[0] | there[1]) && i_hi >= k0 && (MODE == DENSE || i_lo - (k0 + 63) <= P.l)) {      // some pair may be attended
+          const bool some_not = MODE == DENSE || (there[0] & there[1]) != ~0u || i_lo < k0 + 63 || i_hi - k0 > P.l;   // some pair may not be
+          auto mask = [&](uint32_t (&x)[16], int g) {
+            if (!some_not) return;
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((there >> e) & 1u) || !near_sees(P.l, pos, k0 + e)) s[e] = 0xFF800000u;   // -inf
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!((there >> e) & 1u) || (unsigned)(back0 - e) > (unsigned)P.l) s[e] = 0xFF800000u;
+            for (int e = 0; e < 16; ++e) {
+              const bool sees = MODE == DENSE ? near_sees(P.l, pos, k0 + 16 * g + e) : (unsigned)(pos - k0 - 16 * g - e) <= (unsigned)P.l;
+              if (!((there[g >> 1] >> (16 * (g & 1) + e)) & 1u) || !sees) x[e] = 0xFF800000u;   // -inf
             }
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          };
+          // Weights against the reference as it is.  Their sum tells whether a score lies too far above it, which is seldom, so nobody looks for the
+          // maximum first (64 comparisons a thread); a row without a reference does
+          float sum;
+#pragma unroll 1
+          for (int pass = 0;; ++pass) {
+            const float nm = -mst_paged::reference(m);
+            float add[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t x[2][16];
+            tmem_ld16_nowait(t_s, x[0]);
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) mx[(e >> 1) & 3] = fmaxf(mx[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * P.scale_log2;
-          const bool up = top > m + LAZY;                    // a first key (m = -inf) always moves the reference
-          if (__any_sync(0xffffffffu, up)) {
-            const float c = up ? ex2(m - top) : 1.f;         // 0 where nothing has been summed yet
+            for (int g = 0; g < 4; ++g) {
+              tmem_ld16_wait(x[g & 1]);
+              if (g < 3) tmem_ld16_nowait(t_s + 16u * (g + 1), x[(g + 1) & 1]);
+              mask(x[g & 1], g);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float lo = ex2(fmaf(__uint_as_float(x[g & 1][2 * e]), P.scale_log2, nm));
+                const float hi = ex2(fmaf(__uint_as_float(x[g & 1][2 * e + 1]), P.scale_log2, nm));
+                add[e & 1] += lo;
+                add[2 + (e & 1)] += hi;
+                w[8 * g + e] = pack_bf16(lo, hi);
+              }
+            }
+            sum = (add[0] + add[1]) + (add[2] + add[3]);
+            if (pass == 1 || !__any_sync(0xffffffffu, sum > MOST || (live && m == -INFINITY))) break;
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+              uint32_t x[16];
+              tmem_ld16_nowait(t_s + 16u * g, x);
+              tmem_ld16_wait(x);
+              mask(x, g);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) top = fmaxf(top, __uint_as_float(x[e]));
+            }
+            top *= P.scale_log2;
+            const bool up = top > m && (sum > MOST || m == -INFINITY);
+            const float f = up ? ex2(m - top) : 1.f;       // 0 where nothing has been summed yet
             const bool summed = up && m != -INFINITY;
             if (up) m = top;
-            sum2 = mul2(sum2, pack2(c, c));
-            if (__any_sync(0xffffffffu, summed)) {           // this half's outputs so far, once the tile before has been added
-              ok = j == 0 || wait_on(o_done, (n - 1) & 1u, abort_flag);   // the first tile: sums of the strided keys
-              if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-              tc_fence_after();
+            total_w *= f;
+            // the outputs so far are complete: the scores of this tile were issued behind the products of the tile before
+            if (__any_sync(0xffffffffu, summed)) {
 #pragma unroll 1
               for (int g = 0; g < D_; g += 16) {
                 uint32_t v[16];
                 tmem_ld16_nowait(t_out + (uint32_t)g, v);
                 tmem_ld16_wait(v);
-                uint32_t lo[8], hi[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  lo[e] = __float_as_uint(__uint_as_float(v[e]) * c);
-                  hi[e] = __float_as_uint(__uint_as_float(v[e + 8]) * c);
-                }
-                tmem_st8(t_out + (uint32_t)g, lo);
-                tmem_st8(t_out + (uint32_t)(g + 8), hi);
+                for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
+                tmem_st16(t_out + (uint32_t)g, v);
               }
             }
           }
-          const float nm = -mst_paged::reference(m);
-          const uint64_t nm2 = pack2(nm, nm);
-          uint64_t part[2] = {0ULL, 0ULL};
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint64_t p = ex2_2(fma2(pack2(s[2 * e], s[2 * e + 1]), scale2, nm2));
-            part[e & 1] = add2(part[e & 1], p);
-            w[e] = pack_bf16_2(p);
-          }
-          sum2 = add2(sum2, add2(part[0], part[1]));
+          total_w += sum;
         } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) w[e] = 0u;
+          for (int e = 0; e < 32; ++e) w[e] = 0u;
         }
-        tmem_st16(t_s, w);
-        tmem_st_wait();
+        tmem_st32(t_s, w);
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 8 * (n & 1u));
+        if (lane == 0) mbar_arrive(p_full + 8 * half);
       }
       // the two softmaxes of a row meet: weights 2^(m_k - m), over the sum where the row is complete
-      float s_lo, s_hi;
-      unpack2(sum2, s_lo, s_hi);
       stat[half * 2 * ROWS + r] = m;
-      stat[half * 2 * ROWS + ROWS + r] = s_lo + s_hi;
+      stat[half * 2 * ROWS + ROWS + r] = total_w;
       softmax_warps_meet();
       const float ma = stat[r], mb = stat[2 * ROWS + r];
       const float mm = fmaxf(ma, mb);
@@ -492,8 +579,8 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         a0 *= inv;
         a1 *= inv;
       }
-      ok = ok && wait_on(acc_full, lap & 1u, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
+      wait_on(acc_full, lap & 1u, abort_flag);
+      const bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
       tc_fence_after();
       const int t = live ? (T.row0 + r) / P.group : 0, h = kvh * P.group + (live ? (T.row0 + r) % P.group : 0);
       const int64_t token = T.first + t, at = ((int64_t)split * P.B.tokens + token) * P.heads + h;
@@ -550,7 +637,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         for (int rr = warp; rr < T.rows; rr += CW) {
           if (!((again[rr >> 5] >> (rr & 31)) & 1u)) continue;
           float o[D_ / 32], gm, gs;
-          const int64_t to_key = (int64_t)key0 + (int64_t)near * TS;
+          const int64_t to_key = (int64_t)key0 + (int64_t)near * KEYS;
           const int64_t tk = T.first + (T.row0 + rr) / P.group;
           const int hh = kvh * P.group + (T.row0 + rr) % P.group;
           row_again<D_>(P, b, (int)tk, hh, T.p_lo + (T.row0 + rr) / P.group - T.t_lo, key0, have < to_key ? have : (int)to_key, P.l, MODE == DENSE, m0, m1, o,
@@ -572,7 +659,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       }
       fence_async_smem();           // the own rows' place is written by the next tile's copy
     }
-    if (__syncthreads_or(!ok || *abort_flag)) break;      // everybody is done with this tile of rows
+    if (__syncthreads_or(*abort_flag != 0)) break;        // everybody is done with this tile of rows
     ++lap;
     if (MODE == FAR && m1 > m0) ++far_lap;
     base_t += (uint32_t)near;
@@ -637,7 +724,7 @@ mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorM
 template <int D_>
 mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
   const int64_t reach = (int64_t)A.P.B.table_stride * A.P.C.page_size;
-  if (A.P.l < KEYS_OF_TILE) return launch<D_, DENSE>(A, tmQ, tmK, tmV, s);
+  if (A.P.l < DENSE_BELOW) return launch<D_, DENSE>(A, tmQ, tmK, tmV, s);
   // lengths beyond the table's room may still have rows two strides in, which are formed again key by key
   return reach / 2 < A.P.l ? launch<D_, NEAR>(A, tmQ, tmK, tmV, s) : launch<D_, FAR>(A, tmQ, tmK, tmV, s);
 }

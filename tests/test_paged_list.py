@@ -9,6 +9,7 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BIG = 1 << 40
+TILE = 128
 
 
 @pytest.fixture(scope="module")
@@ -94,7 +95,7 @@ def test_tiles_of_many_rows_look_at_their_sets(lib, n, length, group, R, stride)
             assert n0 == end and m0 == m_end and m1 >= m0 and split < active <= 3 and (n1 > n0 or near == 0)
             end, m_end = n1, m1
             for p in positions:
-                seen[p] += [k for k in range(first + 64 * n0, first + 64 * n1) if lib.near(*args, p, k)]
+                seen[p] += [k for k in range(first + TILE * n0, first + TILE * n1) if lib.near(*args, p, k)]
                 seen[p] += [p - m * stride for m in range(m0, m1) if p - m * stride >= 0]
             split += 1
         assert end == near and m_end == 2 + far and split == active
@@ -113,10 +114,10 @@ def test_tiles_of_lengths_that_make_no_sense(lib, length, stride, reach):
     out = (ctypes.c_int32 * 8)()
     assert lib.walk_of(*_args(0, 300, length, 1, stride, reach, 1, 128), 16, 4, 0, out) == 1
     first, near, far, n0, n1, m0, m1, active = list(out)
-    assert first >= 0 and first % 64 == 0 and 0 <= near <= 1 << 25 and far >= 0 and 1 <= active <= 16 and (near > 0) == (length > 300 - 128 - 128)
-    assert first + 64 * near <= max(length, 0) + 64
+    assert first >= 0 and first % TILE == 0 and 0 <= near <= (1 << 31) // TILE and far >= 0 and 1 <= active <= 16 and (near > 0) == (length > 300 - 128 - 128)
+    assert first + TILE * near <= max(length, 0) + TILE
     if reach < length:
-        assert near <= max(1, reach // 64 + 1)
+        assert near <= max(1, reach // TILE + 1)
 
 
 def test_rows_stay_within_the_table(lib):
