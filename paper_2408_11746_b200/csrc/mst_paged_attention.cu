@@ -22,8 +22,8 @@ constexpr int RW = 4;             // warps
 constexpr int RING = 3;
 template <int D>
 struct RowsShape {
-  static constexpr int KEYS = 2048 / D;                   // of a step: 32 or 16
-  static constexpr int STEP_BYTES = KEYS * D * 2;         // 4 KiB each of K and V
+  static constexpr int KEYS = 16;                         // of a step
+  static constexpr int STEP_BYTES = KEYS * D * 2;
   static constexpr int WARP_BYTES = RING * 2 * STEP_BYTES;
   static constexpr int SMEM = RW * WARP_BYTES + 128;
 };
@@ -34,18 +34,18 @@ __device__ __forceinline__ uint32_t piece(uint32_t base, int row, int p) {
 }
 
 template <int D, int MT>
-__global__ void __launch_bounds__(32 * RW) paged_rows_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kernel(const __grid_constant__ Params P) {
   constexpr int R = 16 * MT, KEYS = RowsShape<D>::KEYS, STEP = RowsShape<D>::STEP_BYTES, PIECES = D / 8, AT_ONCE = 32 / PIECES;
   extern __shared__ unsigned char smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
-  const int split = blockIdx.x, b = blockIdx.z;
-  const int kvh = blockIdx.y % P.C.kv_heads;
+  // heads first: blocks that run side by side read neighbouring rows of the same pages
+  const int kvh = (int)blockIdx.x % P.C.kv_heads, split = (int)blockIdx.x / P.C.kv_heads, b = blockIdx.z;
   const uint32_t ring = ((smem_u32(smem_raw) + 127u) & ~127u) + (uint32_t)(warp * RowsShape<D>::WARP_BYTES);
   float* join = reinterpret_cast<float*>(smem_raw + (((smem_u32(smem_raw) + 127u) & ~127u) - smem_u32(smem_raw)));
   __shared__ float stat[RW][R][2];
-  for (int tile = blockIdx.y / P.C.kv_heads;; tile += gridDim.y / P.C.kv_heads) {
+  for (int tile = blockIdx.y;; tile += gridDim.y) {
     List T;
     if (!locate(T, P, b, tile, R)) return;
     uint32_t lo, hi;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(32 * RW) paged_rows_kernel(const __grid_consta
     Key keys[RING], next = {-1, -1};
     int64_t next_at = 0;
     auto look = [&](uint32_t s) {
-      const uint64_t n = (uint64_t)lo + ((uint64_t)s * RW + warp) * KEYS + (KEYS == 32 ? lane : lane % 16);
+      const uint64_t n = (uint64_t)lo + ((uint64_t)s * RW + warp) * KEYS + lane % KEYS;
       next = n < hi ? T.key((uint32_t)n) : Key{-1, -1};
       next_at = 0;
       if (next.pos >= 0) {
@@ -303,19 +303,43 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
     T.range(P.splits, P.least, UNIT, 0, lo, hi, active);
   }
   if (active == 1) return;
+  // lane s: ranges s and s + 32 (there are 64 at most)
   const int64_t step = (int64_t)P.B.tokens * P.heads, at = token * P.heads + h;
-  float mm = -INFINITY;
-#pragma unroll 4
-  for (int s = 0; s < active; ++s) mm = fmaxf(mm, P.part_m[(at + s * step) * 2]);
-  float sum = 0.f, o[E];
+  float2 stat[2] = {make_float2(-INFINITY, 0.f), make_float2(-INFINITY, 0.f)};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (lane + 32 * u < active) stat[u] = *reinterpret_cast<const float2*>(P.part_m + (at + (lane + 32 * u) * step) * 2);
+  float mm = fmaxf(stat[0].x, stat[1].x);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
+  const float c0 = ex2(stat[0].x - reference(mm)), c1 = ex2(stat[1].x - reference(mm));
+  const float sum = warp_sum(fmaf(c0, stat[0].y, c1 * stat[1].y));
+  float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < active; ++s) {
-    const float c = ex2(P.part_m[(at + s * step) * 2] - reference(mm));
-    sum = fmaf(c, P.part_m[(at + s * step) * 2 + 1], sum);
+  for (int s0 = 0; s0 < active; s0 += 8) {
+    float v[8][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(c, P.part_o[(at + s * step) * D + lane * E + e], o[e]);
+    for (int u = 0; u < 8; ++u) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[u][e] = 0.f;
+      if (s0 + u < active) {
+        const float2* from = reinterpret_cast<const float2*>(P.part_o + (at + (s0 + u) * step) * D + lane * E);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 x = from[e / 2];
+          v[u][e] = x.x;
+          v[u][e + 1] = x.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float c = __shfl_sync(0xffffffffu, s0 + u < 32 ? c0 : c1, (s0 + u) & 31);
+      if (s0 + u < active)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(c, v[u][e], o[e]);
+    }
   }
   finish<E>(P, token, h, lane, o, mm, sum);
 }
@@ -329,10 +353,10 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   const int64_t lists = (int64_t)(b.batch > 0 ? b.batch : 1) * c.kv_heads;
   p.tiles = rows >= TILES_FROM && group <= TILE_ROWS && (int64_t)c.kv_heads * 64 < 0x7FFFFFFF;
   p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 16 ? 16 : 32;
-  const int64_t tiles = (rows + p.rows - 1) / p.rows, most = p.tiles ? 65535 : 65535 / c.kv_heads;
+  const int64_t tiles = (rows + p.rows - 1) / p.rows, most = 65535;
   p.count = (int)(tiles < most ? tiles : most);
   // units of the longest list: 64 entries, or tiles of 128 keys
-  const int64_t nt = (p.rows + group - 1) / group;
+  const int64_t in_tile = (p.rows + group - 1) / group, nt = b.max_new < in_tile ? (b.max_new > 0 ? b.max_new : 1) : in_tile;
   int64_t units;
   if (p.tiles) {
     units = (stride >= len || stride < DENSE_BELOW ? len : stride + nt < len ? stride + nt : len) / KEYS_OF_TILE + 1;
@@ -340,7 +364,7 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   } else {
     const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
     units = (list + UNIT - 1) / UNIT;
-    p.least = 4;
+    p.least = 8;
   }
   const int64_t blocks = lists * tiles, want = (p.tiles ? 8 : 12) * (int64_t)mst_sm_count();
   int64_t splits = (want + blocks - 1) / blocks;
@@ -362,8 +386,8 @@ template <int D, int MT>
 mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
   const size_t smem = RowsShape<D>::SMEM;
   MST_SMEM_LIMIT((paged_rows_kernel<D, MT>), smem);
-  const unsigned y = (unsigned)(plan.count * P.C.kv_heads), z = (unsigned)P.B.batch;
-  MST_CUDA_TRY(mst_launch_overlapped(paged_rows_kernel<D, MT>, dim3((unsigned)plan.splits, y, z), dim3(32 * RW), smem, s, P));
+  const dim3 grid((unsigned)(plan.splits * P.C.kv_heads), (unsigned)plan.count, (unsigned)P.B.batch);
+  MST_CUDA_TRY(mst_launch_overlapped(paged_rows_kernel<D, MT>, grid, dim3(32 * RW), smem, s, P));
   return MST_OK;
 }
 template <int D>
