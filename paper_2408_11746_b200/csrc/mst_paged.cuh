@@ -12,6 +12,7 @@ struct Cache {
   __nv_bfloat16 *K, *V;
   int64_t page_stride, token_stride, head_stride;
   int num_pages, page_size, kv_heads, D;
+  Divider by_page;
 };
 struct Batch {
   const int32_t *first, *len, *table;
@@ -36,7 +37,7 @@ inline mst_status_t check(const mst_paged_cache_t* c, const mst_paged_batch_t* b
       ((reinterpret_cast<uintptr_t>(b->first) | reinterpret_cast<uintptr_t>(b->len) | reinterpret_cast<uintptr_t>(b->page_table)) & 3u) != 0)
     return MST_ERR_SHAPE;
   *cache = Cache{(__nv_bfloat16*)c->K, (__nv_bfloat16*)c->V, c->page_stride, c->token_stride, c->head_stride,
-                 c->num_pages, c->page_size, c->kv_heads, c->head_dim};
+                 c->num_pages, c->page_size, c->kv_heads, c->head_dim, Divider::of((uint32_t)c->page_size)};
   *batch = Batch{b->first, b->len, b->page_table, b->batch, b->tokens, b->table_stride};
   return MST_OK;
 }
@@ -49,7 +50,7 @@ struct Slot {
 // Slot of position p (p >= 0) of sequence b.  `flag`: the file's own word for pages that do not exist
 __device__ __forceinline__ Slot slot_of(const Cache& C, const Batch& B, int b, int p, int* flag) {
   int slot;
-  const int id = page_of(B.table + (int64_t)b * B.table_stride, B.table_stride, C.page_size, C.num_pages, p, slot);
+  const int id = page_of(B.table + (int64_t)b * B.table_stride, B.table_stride, C.by_page, C.num_pages, p, slot);
   if (id < 0) {
     *flag = 1;
     return Slot{false, 0};

@@ -15,15 +15,16 @@ __device__ __forceinline__ uint32_t steps_below(uint32_t f, uint32_t t, uint32_t
 
 // ---------------------------------------------------------------------------------------------- few rows
 // Four warps go through a range of the list, each through every fourth step of it with a ring of its own (no block-wide step until the
-// end): K and V rows of a step come in by 16-byte asynchronous copies, two steps ahead; scores and weighted sums by warp-level products
-// with the tile's rows in a 16-row operand, which costs less than the rows' bytes take to arrive however few of the 16 there are.  The
-// warps' softmaxes are joined through shared memory, ranges by a second launch.
+// end): K and V rows of a step come in by 16-byte asynchronous copies, two steps ahead, and where they are is looked up a step before that.
+// Products are warp-level with the keys as the 16 rows of the left operand, S^T = K Q^T and O^T = V^T P^T, so that queries come in eights:
+// of the few there are, none pays for more than seven that are not there (with the queries on the left, in sixteens, a step of 16 keys took 366
+// instructions, and the long-context case 46 us).  The warps' softmaxes are joined through shared memory, ranges by a second launch.
 constexpr int RW = 4;             // warps
 constexpr int RING = 3;
 template <int D>
 struct RowsShape {
-  static constexpr int KEYS = 16;                         // of a step
-  static constexpr int STEP_BYTES = KEYS * D * 2;
+  static constexpr int KEYS = 2048 / D;                   // of a step: 32 or 16
+  static constexpr int STEP_BYTES = KEYS * D * 2;         // 4 KiB each of K and V
   static constexpr int WARP_BYTES = RING * 2 * STEP_BYTES;
   static constexpr int SMEM = RW * WARP_BYTES + 128;
 };
@@ -32,12 +33,19 @@ template <int D>
 __device__ __forceinline__ uint32_t piece(uint32_t base, int row, int p) {
   return base + (uint32_t)(row * D * 2) + (((uint32_t)p ^ (uint32_t)(row & 7)) << 4);
 }
+// an 8 x 8 matrix of 16-bit values spread over the warp, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t t;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
+  return t;
+}
 
-template <int D, int MT>
-__global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kernel(const __grid_constant__ Params P) {
-  constexpr int R = 16 * MT, KEYS = RowsShape<D>::KEYS, STEP = RowsShape<D>::STEP_BYTES, PIECES = D / 8, AT_ONCE = 32 / PIECES;
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_constant__ Params P) {
+  constexpr int R = 8 * NT, KEYS = RowsShape<D>::KEYS, STEP = RowsShape<D>::STEP_BYTES, PIECES = D / 8, AT_ONCE = 32 / PIECES, G16 = KEYS / 16;
+  constexpr uint32_t NOWHERE = 0xffffffffu;
   extern __shared__ unsigned char smem_raw[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & 3, mrow = lane >> 2;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
   // heads first: blocks that run side by side read neighbouring rows of the same pages
@@ -51,59 +59,36 @@ __global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kern
     uint32_t lo, hi;
     int active;
     if (!T.range(P.splits, P.least, UNIT, split, lo, hi, active)) continue;
-    // queries: the 16 x 16 operand's published layout (row lane / 4 and + 8, columns 2 (lane % 4) and + 8)
-    uint32_t q[MT][D / 16][4];
-    int pos[MT][2], tok[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int r = mt * 16 + u * 8 + lane / 4, rr = r < T.rows ? r : 0;
-        const int t = (T.row0 + rr) / P.group, h = kvh * P.group + (T.row0 + rr) % P.group;
-        tok[mt][u] = t - T.t_lo;
-        pos[mt][u] = T.p_lo + tok[mt][u];
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(P.Q + (int64_t)(T.first + t) * P.ldq + (int64_t)h * D) + lane % 4;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          q[mt][k][u] = src[k * 8];
-          q[mt][k][u + 2] = src[k * 8 + 4];
-        }
-      }
-    float acc[MT][D / 8][4], m[MT][2], sum[MT][2];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int n = 0; n < D / 8; ++n) acc[mt][n][0] = acc[mt][n][1] = acc[mt][n][2] = acc[mt][n][3] = 0.f;
-      m[mt][0] = m[mt][1] = -INFINITY;
-      sum[mt][0] = sum[mt][1] = 0.f;
-    }
-    // step s of this warp: entries lo + (s RW + warp) KEYS ..; where they are is looked up a step before their copies go out
-    Key keys[RING], next = {-1, -1};
-    int64_t next_at = 0;
+    const uint32_t total = (hi - lo + KEYS - 1) / KEYS;                                // steps of the block
+    const uint32_t mine = total > (uint32_t)warp ? (total - warp + RW - 1) / RW : 0u;
+    // step s of this warp: entries lo + (s RW + warp) KEYS ..; a lane's entry and its place in the cache, in pieces of 16 bytes
+    Key keys[RING], next;
+    uint32_t next_at;
+    const uint32_t head_at = (uint32_t)((int64_t)kvh * P.C.head_stride / 8);
     auto look = [&](uint32_t s) {
       const uint64_t n = (uint64_t)lo + ((uint64_t)s * RW + warp) * KEYS + lane % KEYS;
       next = n < hi ? T.key((uint32_t)n) : Key{-1, -1};
-      next_at = 0;
+      next_at = NOWHERE;
       if (next.pos >= 0) {
         const Slot sl = slot_of(P.C, P.B, b, next.pos, &g_bad_page);
-        if (sl.exists) next_at = sl.at + (int64_t)kvh * P.C.head_stride;
+        if (sl.exists) next_at = (uint32_t)(sl.at / 8) + head_at;
         else next.pos = -1;
       }
     };
     auto load = [&](int slot) {
       keys[slot] = next;
+      const int c = lane % PIECES;
       const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
 #pragma unroll
       for (int r0 = 0; r0 < KEYS; r0 += AT_ONCE) {
-        const int r = r0 + lane / PIECES, c = lane % PIECES;
-        const int64_t a = __shfl_sync(0xffffffffu, next_at, r);
-        const bool there = __shfl_sync(0xffffffffu, next.pos, r) >= 0;
-        cp16(piece<D>(kt, r, c), P.C.K + a + c * 8, there);
-        cp16(piece<D>(vt, r, c), P.C.V + a + c * 8, there);
+        const int r = r0 + lane / PIECES;
+        const uint32_t a = __shfl_sync(0xffffffffu, next_at, r);
+        const bool there = a != NOWHERE;
+        const int64_t from = (int64_t)(there ? a + (uint32_t)c : 0u) * 8;
+        cp16(piece<D>(kt, r, c), P.C.K + from, there);
+        cp16(piece<D>(vt, r, c), P.C.V + from, there);
       }
     };
-    const uint32_t total = (hi - lo + KEYS - 1) / KEYS;                                // steps of the block
-    const uint32_t mine = total > (uint32_t)warp ? (total - warp + RW - 1) / RW : 0u;
 #pragma unroll
     for (int s = 0; s < RING - 1; ++s) {
       look((uint32_t)s);
@@ -111,6 +96,34 @@ __global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kern
       cp_commit();
     }
     look(RING - 1);
+    // queries: the right operand's published layout (column lane / 4, rows 2 (lane % 4) and + 8)
+    uint32_t q[NT][D / 16][2];
+    int pos[NT][2], tok[NT][2];     // of the rows whose scores the lane holds: 2 (lane % 4) and the next
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int r = nt * 8 + 2 * col + u;
+        const int t = P.by_group.over(T.row0 + (r < T.rows ? r : 0));
+        tok[nt][u] = t - T.t_lo;
+        pos[nt][u] = T.p_lo + tok[nt][u];
+      }
+      const int r = nt * 8 + mrow, at = T.row0 + (r < T.rows ? r : 0), t = P.by_group.over(at), h = kvh * P.group + at - t * P.group;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(P.Q + (int64_t)(T.first + t) * P.ldq + (int64_t)h * D) + col;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        q[nt][k][0] = src[k * 8];
+        q[nt][k][1] = src[k * 8 + 4];
+      }
+    }
+    float acc[NT][D / 16][4], m[NT][2], sum[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) acc[nt][d][0] = acc[nt][d][1] = acc[nt][d][2] = acc[nt][d][3] = 0.f;
+      m[nt][0] = m[nt][1] = -INFINITY;
+      sum[nt][0] = sum[nt][1] = 0.f;
+    }
     for (uint32_t s0 = 0; s0 < mine; s0 += RING) {
 #pragma unroll
       for (int slot = 0; slot < RING; ++slot) {
@@ -124,117 +137,110 @@ __global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kern
         }
         cp_commit();
         const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
-        float x[MT][KEYS / 8][4];
+        float x[NT][G16][4];               // keys lane / 4 and + 8 of each sixteen, rows 2 (lane % 4) and the next
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int g = 0; g < G16; ++g) {
 #pragma unroll
-          for (int n = 0; n < KEYS / 8; ++n) x[mt][n][0] = x[mt][n][1] = x[mt][n][2] = x[mt][n][3] = 0.f;
+          for (int nt = 0; nt < NT; ++nt) x[nt][g][0] = x[nt][g][1] = x[nt][g][2] = x[nt][g][3] = 0.f;
 #pragma unroll
-        for (int n = 0; n < KEYS / 8; ++n)
-#pragma unroll
-          for (int k2 = 0; k2 < D / 32; ++k2) {
+          for (int k = 0; k < D / 16; ++k) {
             uint32_t f[4];
-            ldsm_x4(f, piece<D>(kt, n * 8 + (lane & 7), k2 * 4 + (lane >> 3)));
+            ldsm_x4(f, piece<D>(kt, g * 16 + (lane & 15), k * 2 + (lane >> 4)));
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma_bf16(x[mt][n], q[mt][2 * k2], f[0], f[1]);
-              mma_bf16(x[mt][n], q[mt][2 * k2 + 1], f[2], f[3]);
-            }
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(x[nt][g], f, q[nt][k][0], q[nt][k][1]);
           }
+        }
         const Key key = keys[slot];
         const bool all = key.pos >= 0 && (key.who >= 0 ? T.nt == 1 : key.pos <= T.p_lo && T.p_hi - key.pos < T.l);
         if (!__all_sync(0xffffffffu, all)) {
 #pragma unroll
-          for (int n = 0; n < KEYS / 8; ++n)
+          for (int g = 0; g < G16; ++g)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int from = n * 8 + 2 * (lane & 3) + e;
+              const int from = g * 16 + 8 * e + mrow;
               const Key k = {__shfl_sync(0xffffffffu, key.pos, from), __shfl_sync(0xffffffffu, key.who, from)};
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt)
+              for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
-                  if (!T.sees(pos[mt][u], tok[mt][u], k)) x[mt][n][2 * u + e] = -INFINITY;
+                  if (!T.sees(pos[nt][u], tok[nt][u], k)) x[nt][g][2 * e + u] = -INFINITY;
             }
         }
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int nt = 0; nt < NT; ++nt) {
           float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int n = 0; n < KEYS / 8; ++n)
+          for (int g = 0; g < G16; ++g)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) top[u] = fmaxf(top[u], fmaxf(x[mt][n][2 * u], x[mt][n][2 * u + 1]));
+            for (int u = 0; u < 2; ++u) top[u] = fmaxf(top[u], fmaxf(x[nt][g][u], x[nt][g][2 + u]));
           top[0] *= P.scale_log2;
           top[1] *= P.scale_log2;
-          if (__any_sync(0xffffffffu, top[0] > m[mt][0] + LAZY || top[1] > m[mt][1] + LAZY)) {
+          if (__any_sync(0xffffffffu, top[0] > m[nt][0] + LAZY || top[1] > m[nt][1] + LAZY)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
-              top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 2));
-              const bool up = top[u] > m[mt][u] + LAZY;
-              const float c = up ? ex2(m[mt][u] - top[u]) : 1.f;
-              if (up) m[mt][u] = top[u];
-              sum[mt][u] *= c;
 #pragma unroll
-              for (int n = 0; n < D / 8; ++n) {
-                acc[mt][n][2 * u] *= c;
-                acc[mt][n][2 * u + 1] *= c;
+              for (int d = 4; d < 32; d *= 2) top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], d));
+              const bool up = top[u] > m[nt][u] + LAZY;
+              const float c = up ? ex2(m[nt][u] - top[u]) : 1.f;
+              if (up) m[nt][u] = top[u];
+              sum[nt][u] *= c;
+#pragma unroll
+              for (int d = 0; d < D / 16; ++d) {
+                acc[nt][d][u] *= c;
+                acc[nt][d][2 + u] *= c;
               }
             }
           }
-          const float r0 = reference(m[mt][0]), r1 = reference(m[mt][1]);
+          const float r0 = reference(m[nt][0]), r1 = reference(m[nt][1]);
 #pragma unroll
-          for (int n = 0; n < KEYS / 8; ++n) {
-            x[mt][n][0] = ex2(fmaf(x[mt][n][0], P.scale_log2, -r0));
-            x[mt][n][1] = ex2(fmaf(x[mt][n][1], P.scale_log2, -r0));
-            x[mt][n][2] = ex2(fmaf(x[mt][n][2], P.scale_log2, -r1));
-            x[mt][n][3] = ex2(fmaf(x[mt][n][3], P.scale_log2, -r1));
-            sum[mt][0] += x[mt][n][0] + x[mt][n][1];
-            sum[mt][1] += x[mt][n][2] + x[mt][n][3];
-          }
-        }
+          for (int g = 0; g < G16; ++g) {
 #pragma unroll
-        for (int k = 0; k < KEYS / 16; ++k) {
-          uint32_t a[MT][4];
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            a[mt][0] = pack_bf16(x[mt][2 * k][0], x[mt][2 * k][1]);
-            a[mt][1] = pack_bf16(x[mt][2 * k][2], x[mt][2 * k][3]);
-            a[mt][2] = pack_bf16(x[mt][2 * k + 1][0], x[mt][2 * k + 1][1]);
-            a[mt][3] = pack_bf16(x[mt][2 * k + 1][2], x[mt][2 * k + 1][3]);
-          }
-#pragma unroll
-          for (int n2 = 0; n2 < D / 16; ++n2) {
-            uint32_t f[4];
-            ldsm_x4_t(f, piece<D>(vt, k * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, n2 * 2 + (lane >> 4)));
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma_bf16(acc[mt][2 * n2], a[mt], f[0], f[1]);
-              mma_bf16(acc[mt][2 * n2 + 1], a[mt], f[2], f[3]);
+            for (int e = 0; e < 2; ++e) {
+              x[nt][g][2 * e] = ex2(fmaf(x[nt][g][2 * e], P.scale_log2, -r0));
+              x[nt][g][2 * e + 1] = ex2(fmaf(x[nt][g][2 * e + 1], P.scale_log2, -r1));
             }
+            sum[nt][0] += x[nt][g][0] + x[nt][g][2];
+            sum[nt][1] += x[nt][g][1] + x[nt][g][3];
           }
         }
-        __syncwarp();
+#pragma unroll
+        for (int g = 0; g < G16; ++g) {
+          uint32_t w[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            w[nt][0] = transposed(pack_bf16(x[nt][g][0], x[nt][g][1]));
+            w[nt][1] = transposed(pack_bf16(x[nt][g][2], x[nt][g][3]));
+          }
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) {
+            uint32_t f[4];
+            ldsm_x4_t(f, piece<D>(vt, g * 16 + (lane & 7) + (lane >> 4) * 8, d * 2 + ((lane >> 3) & 1)));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][d], f, w[nt][0], w[nt][1]);
+          }
+        }
       }
     }
     cp_wait<0>();
     // the warps' softmaxes meet in the rings' place
     __syncthreads();
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int r = mt * 16 + u * 8 + lane / 4;
-        float v = sum[mt][u];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        if ((lane & 3) == 0) {
-          stat[warp][r][0] = m[mt][u];
+        const int r = nt * 8 + 2 * col + u;
+        float v = sum[nt][u];
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (mrow == 0) {
+          stat[warp][r][0] = m[nt][u];
           stat[warp][r][1] = v;
         }
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n)
-          *reinterpret_cast<float2*>(join + ((warp * R + r) * D + n * 8 + 2 * (lane & 3))) = make_float2(acc[mt][n][2 * u], acc[mt][n][2 * u + 1]);
+        for (int d = 0; d < D / 16; ++d) {
+          join[(warp * R + r) * D + d * 16 + mrow] = acc[nt][d][u];
+          join[(warp * R + r) * D + d * 16 + 8 + mrow] = acc[nt][d][2 + u];
+        }
       }
     static_assert(RW * R * D * 4 <= RowsShape<D>::SMEM - 128, "the sums fit the rings");
     __syncthreads();
@@ -255,14 +261,14 @@ __global__ void __launch_bounds__(32 * RW, D == 64 ? 4 / MT : 2) paged_rows_kern
       bool bad = !(total_w * 0.f == 0.f);
 #pragma unroll
       for (int e = 0; e < E; ++e) bad = bad || !(o[e] * 0.f == 0.f);
+      const int t = P.by_group.over(T.row0 + r), h = kvh * P.group + T.row0 + r - t * P.group;
+      const int64_t token = T.first + t;
       if (__any_sync(0xffffffffu, bad)) {
         const uint32_t w_lo = lo < T.W ? lo : T.W, w_hi = hi < T.W ? hi : T.W, f_lo = lo - w_lo, f_hi = hi - w_hi;   // of the window, behind it
-        const uint32_t t_in = (uint32_t)((T.row0 + r) / P.group - T.t_lo), nt = (uint32_t)T.nt;
-        row_again<D>(P, b, T.first + (T.row0 + r) / P.group, kvh * P.group + (T.row0 + r) % P.group, T.p_lo + (int)t_in, T.w0 + (int)w_lo, T.w0 + (int)w_hi,
-                     T.l - 1, T.dense, 1 + (int)steps_below(f_lo, t_in, nt), 1 + (int)steps_below(f_hi, t_in, nt), o, mm, total_w);
+        const uint32_t t_in = (uint32_t)(t - T.t_lo), nt = (uint32_t)T.nt;
+        row_again<D>(P, b, (int)token, h, T.p_lo + (int)t_in, T.w0 + (int)w_lo, T.w0 + (int)w_hi, T.l - 1, T.dense, 1 + (int)steps_below(f_lo, t_in, nt),
+                     1 + (int)steps_below(f_hi, t_in, nt), o, mm, total_w);
       }
-      const int t = (T.row0 + r) / P.group, h = kvh * P.group + (T.row0 + r) % P.group;
-      const int64_t token = T.first + t;
       if (active == 1) {
         finish<E>(P, token, h, lane, o, mm, total_w);
       } else {
@@ -352,7 +358,7 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   const int64_t rows = (int64_t)(b.max_new > 0 ? b.max_new : 1) * group, len = b.max_len > 0 ? b.max_len : 1;
   const int64_t lists = (int64_t)(b.batch > 0 ? b.batch : 1) * c.kv_heads;
   p.tiles = rows >= TILES_FROM && group <= TILE_ROWS && (int64_t)c.kv_heads * 64 < 0x7FFFFFFF;
-  p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 16 ? 16 : 32;
+  p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + p.rows - 1) / p.rows, most = 65535;
   p.count = (int)(tiles < most ? tiles : most);
   // units of the longest list: 64 entries, or tiles of 128 keys
@@ -382,13 +388,17 @@ size_t workspace_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int 
   return (size_t)p.splits * (size_t)b.tokens * (size_t)heads * (size_t)(c.head_dim + 2) * sizeof(float);
 }
 
-template <int D, int MT>
+template <int D, int NT>
 mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
   const size_t smem = RowsShape<D>::SMEM;
-  MST_SMEM_LIMIT((paged_rows_kernel<D, MT>), smem);
+  MST_SMEM_LIMIT((paged_rows_kernel<D, NT>), smem);
   const dim3 grid((unsigned)(plan.splits * P.C.kv_heads), (unsigned)plan.count, (unsigned)P.B.batch);
-  MST_CUDA_TRY(mst_launch_overlapped(paged_rows_kernel<D, MT>, grid, dim3(32 * RW), smem, s, P));
+  MST_CUDA_TRY(mst_launch_overlapped(paged_rows_kernel<D, NT>, grid, dim3(32 * RW), smem, s, P));
   return MST_OK;
+}
+template <int D>
+mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
+  return plan.rows == 8 ? launch_rows<D, 1>(P, plan, s) : plan.rows == 16 ? launch_rows<D, 2>(P, plan, s) : launch_rows<D, 4>(P, plan, s);
 }
 template <int D>
 mst_status_t launch_join(const Params& P, const Plan& plan, cudaStream_t s) {
@@ -403,6 +413,10 @@ mst_status_t check_attention(const mst_paged_cache_t* cache, const mst_paged_bat
   if (heads <= 0 || stride <= 0) return MST_ERR_INVALID_ARG;
   if (heads % cache->kv_heads != 0 || heads > 65535) return MST_ERR_SHAPE;
   if (cache->head_dim != 64 && cache->head_dim != 128) return MST_ERR_SHAPE;
+  // places in the cache are 32-bit numbers of 16-byte pieces
+  if (((int64_t)cache->num_pages - 1) * (cache->page_stride / 8) + ((int64_t)cache->page_size - 1) * (cache->token_stride / 8) +
+          ((int64_t)cache->kv_heads - 1) * (cache->head_stride / 8) + cache->head_dim / 8 >= 0xFFFFFFFFLL)
+    return MST_ERR_SHAPE;
   return MST_OK;
 }
 
@@ -452,6 +466,7 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   P.ldo = ldo;
   P.heads = heads;
   P.group = heads / cache->kv_heads;
+  P.by_group = Divider::of((uint32_t)P.group);
   P.l = stride;
   P.scale_log2 = LOG2E / sqrtf((float)cache->head_dim);
   P.splits = plan.splits;
@@ -460,8 +475,7 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   if (need) P.part_m = P.part_o + (size_t)plan.splits * (size_t)batch->tokens * (size_t)heads * (size_t)cache->head_dim;
   cudaStream_t s = (cudaStream_t)stream;
   if (plan.tiles) MST_TRY(launch_tiles(P, plan, s));
-  else if (cache->head_dim == 64) MST_TRY(plan.rows == 16 ? (launch_rows<64, 1>(P, plan, s)) : (launch_rows<64, 2>(P, plan, s)));
-  else MST_TRY(plan.rows == 16 ? (launch_rows<128, 1>(P, plan, s)) : (launch_rows<128, 2>(P, plan, s)));
+  else MST_TRY(cache->head_dim == 64 ? launch_rows<64>(P, plan, s) : launch_rows<128>(P, plan, s));
   if (plan.splits > 1) MST_TRY(cache->head_dim == 64 ? launch_join<64>(P, plan, s) : launch_join<128>(P, plan, s));
   return MST_OK;
 }

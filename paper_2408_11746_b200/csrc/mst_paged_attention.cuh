@@ -23,6 +23,7 @@ struct Params {
   float* lse;
   int64_t ldq, ldo;
   int heads, group, l;
+  Divider by_group;
   float scale_log2;
   int splits, least;      // most ranges of a list, and the least units of one (plan)
   float* part_o;          // [splits][tokens * heads][D]: sums against part_m, [splits][tokens * heads][2]: reference and sum of weights
@@ -35,7 +36,7 @@ constexpr int UNIT = 64;  // keys of a list that stay together
 __device__ __forceinline__ bool locate(List& T, const Params& P, int b, int tile, int R) {
   const int len = P.B.len[b];
   const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.group, P.l, reach, tile, R)) return false;
+  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.by_group, P.l, reach, tile, R)) return false;
   if (len > reach) g_bad_page = 1;
   return true;
 }

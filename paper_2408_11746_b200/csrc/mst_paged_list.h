@@ -16,6 +16,25 @@
 
 namespace mst_paged {
 
+// Quotients by a number that stays, of numbers below 2^31, without a division (Granlund and Montgomery 1994: a multiplier rounded up and the quotient's
+// high word, which with the number itself does not pass 32 bits)
+struct Divider {
+  uint32_t d, mul;
+  int shift;
+  static Divider of(uint32_t d) {
+    int l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    return Divider{d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l};
+  }
+  MST_HD int over(int n) const {
+#ifdef __CUDA_ARCH__
+    return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift);
+#else
+    return (int)(((uint32_t)(((uint64_t)mul * (uint32_t)n) >> 32) + (uint32_t)n) >> shift);
+#endif
+  }
+};
+
 struct Key {
   int pos;    // -1: none
   int who;    // the token of the tile that alone looks at it, -1: the window
@@ -32,17 +51,17 @@ struct List {
 
   // Tile `tile` of `R` pairs of a sequence with rows first .. end - 1 of `tokens` and `len` positions, `group` query heads to a key head, `reach`
   // positions that its table has room for.  false: no such tile.
-  MST_HD bool locate(int first_, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R) {
+  MST_HD bool locate(int first_, int end, int len, int tokens, const Divider& group, int stride, int64_t reach, int tile, int R) {
     first = first_;
     l = stride;
     if (first < 0 || end <= first || end > tokens) return false;
     const int n = end - first;
-    const int64_t all = (int64_t)n * group, r0 = (int64_t)tile * R;
-    if (r0 >= all) return false;
+    const int64_t all = (int64_t)n * group.d, r0 = (int64_t)tile * R;
+    if (r0 >= all || r0 + R > 0x7FFFFFFF) return false;
     row0 = (int)r0;
     rows = all - r0 < R ? (int)(all - r0) : R;
-    t_lo = row0 / group;
-    nt = (row0 + rows - 1) / group - t_lo + 1;
+    t_lo = group.over(row0);
+    nt = group.over(row0 + rows - 1) - t_lo + 1;
     const int64_t p = (int64_t)len - n + t_lo;
     p_lo = p < -(1 << 30) ? -(1 << 30) : (int)p;      // a length that far below its tokens: nothing is looked at either way
     p_hi = p_lo + nt - 1;
@@ -123,9 +142,9 @@ MST_HD bool near_sees(int l, int p, int k) {
 }
 
 // Page of position p >= 0 in a sequence's row of the table, -1 where there is none
-MST_HD int page_of(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int& slot) {
-  const int page = p / page_size;
-  slot = p - page * page_size;
+MST_HD int page_of(const int32_t* row, int table_stride, const Divider& page_size, int num_pages, int p, int& slot) {
+  const int page = page_size.over(p);
+  slot = p - page * (int)page_size.d;
   if (page >= table_stride) return -1;
   const int id = row[page];
   return id >= 0 && id < num_pages ? id : -1;

@@ -267,7 +267,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         bool whole = A.box > 0 && KEYS <= have - k0;
         int id = 0, slot = 0;
         const bool mine = whole && lane * A.box < KEYS;
-        if (mine) id = page_of(table, P.B.table_stride, P.C.page_size, P.C.num_pages, k0 + lane * A.box, slot);
+        if (mine) id = page_of(table, P.B.table_stride, P.C.by_page, P.C.num_pages, k0 + lane * A.box, slot);
         whole = whole && __all_sync(0xffffffffu, id >= 0);
         const uint32_t before = (n / STAGES - 1) & 1u;
         if (waiting) {        // ahead of any wait for a slot: the products of the tile before that one may be waiting for these keys

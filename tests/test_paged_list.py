@@ -163,3 +163,12 @@ def test_pages_that_do_not_exist(lib):
     assert lib.page(row.ctypes, 0, 7, 9, 0, ctypes.byref(slot)) == -1
     assert lib.page(row.ctypes, len(row), 1, 9, (1 << 31) - 1, ctypes.byref(slot)) == -1
     assert lib.page(row.ctypes, len(row), 1, 0, 0, ctypes.byref(slot)) == -1
+
+
+def test_quotients_without_division(lib):
+    rng = np.random.default_rng(1)
+    top = (1 << 31) - 1
+    for d in list(range(1, 70)) + [100, 127, 128, 129, 1000, 4096, 65535, 65536, 65537, (1 << 30) - 1, 1 << 30, (1 << 30) + 1, top]:
+        ns = {0, 1, d - 1, d, min(d + 1, top), top, top - 1, top // d * d, max(top // d * d - 1, 0)} | set(rng.integers(0, top, 200).tolist())
+        for n in ns:
+            assert lib.over(ctypes.c_uint32(d), ctypes.c_int(n)) == n // d
