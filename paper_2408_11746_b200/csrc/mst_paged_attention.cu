@@ -61,41 +61,57 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
     if (!T.range(P.splits, P.least, UNIT, split, lo, hi, active)) continue;
     const uint32_t total = (hi - lo + KEYS - 1) / KEYS;                                // steps of the block
     const uint32_t mine = total > (uint32_t)warp ? (total - warp + RW - 1) / RW : 0u;
-    // step s of this warp: entries lo + (s RW + warp) KEYS ..; a lane's entry and its place in the cache, in pieces of 16 bytes
-    Key keys[RING], next;
-    uint32_t next_at;
-    const uint32_t head_at = (uint32_t)((int64_t)kvh * P.C.head_stride / 8);
+    // Step s of this warp: entries lo + (s RW + warp) KEYS ..; places in the cache are numbers of 16-byte pieces.
+    // An entry's page is asked for a step before its number is used: the use would wait for the answer where it stands.
+    Key keys[RING];
+    struct Entry { Key key; int slot, id; };
+    const uint32_t head_at = (uint32_t)((int64_t)kvh * P.C.head_stride / 8), page_step = (uint32_t)(P.C.page_stride / 8), slot_step = (uint32_t)(P.C.token_stride / 8);
+    const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
     auto look = [&](uint32_t s) {
       const uint64_t n = (uint64_t)lo + ((uint64_t)s * RW + warp) * KEYS + lane % KEYS;
-      next = n < hi ? T.key((uint32_t)n) : Key{-1, -1};
-      next_at = NOWHERE;
-      if (next.pos >= 0) {
-        const Slot sl = slot_of(P.C, P.B, b, next.pos, &g_bad_page);
-        if (sl.exists) next_at = (uint32_t)(sl.at / 8) + head_at;
-        else next.pos = -1;
+      Entry e = {n < hi ? T.key((uint32_t)n) : Key{-1, -1}, 0, -1};
+      if (e.key.pos >= 0) {
+        const int page = P.C.by_page.over(e.key.pos);
+        e.slot = e.key.pos - page * P.C.page_size;
+        if (page < P.B.table_stride) e.id = __ldg(table + page);
       }
+      return e;
     };
-    auto load = [&](int slot) {
-      keys[slot] = next;
+    auto load = [&](int slot, Entry e) {
+      uint32_t at = NOWHERE;
+      if (e.key.pos >= 0) {
+        if ((uint32_t)e.id < (uint32_t)P.C.num_pages) {
+          at = (uint32_t)e.id * page_step + (uint32_t)e.slot * slot_step + head_at;
+        } else {
+          e.key.pos = -1;
+          g_bad_page = 1;
+        }
+      }
+      keys[slot] = e.key;
       const int c = lane % PIECES;
       const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
 #pragma unroll
       for (int r0 = 0; r0 < KEYS; r0 += AT_ONCE) {
         const int r = r0 + lane / PIECES;
-        const uint32_t a = __shfl_sync(0xffffffffu, next_at, r);
+        const uint32_t a = __shfl_sync(0xffffffffu, at, r);
         const bool there = a != NOWHERE;
         const int64_t from = (int64_t)(there ? a + (uint32_t)c : 0u) * 8;
         cp16(piece<D>(kt, r, c), P.C.K + from, there);
         cp16(piece<D>(vt, r, c), P.C.V + from, there);
       }
     };
+    Entry next;
+    {
+      Entry ahead[RING];
 #pragma unroll
-    for (int s = 0; s < RING - 1; ++s) {
-      look((uint32_t)s);
-      if ((uint32_t)s < mine) load(s);
-      cp_commit();
+      for (int s = 0; s < RING; ++s) ahead[s] = look((uint32_t)s);
+#pragma unroll
+      for (int s = 0; s < RING - 1; ++s) {
+        if ((uint32_t)s < mine) load(s, ahead[s]);
+        cp_commit();
+      }
+      next = ahead[RING - 1];
     }
-    look(RING - 1);
     // queries: the right operand's published layout (column lane / 4, rows 2 (lane % 4) and + 8)
     uint32_t q[NT][D / 16][2];
     int pos[NT][2], tok[NT][2];     // of the rows whose scores the lane holds: 2 (lane % 4) and the next
@@ -132,8 +148,8 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
         cp_wait<RING - 2>();
         __syncwarp();                      // every lane's copies are in, and the slot to be filled has been read by every lane
         if (s + RING - 1 < mine) {
-          load((slot + RING - 1) % RING);
-          look(s + RING);
+          load((slot + RING - 1) % RING, next);
+          next = look(s + RING);
         }
         cp_commit();
         const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
