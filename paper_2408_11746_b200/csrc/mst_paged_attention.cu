@@ -21,6 +21,7 @@ __device__ __forceinline__ uint32_t steps_below(uint32_t f, uint32_t t, uint32_t
 // instructions, and the long-context case 46 us).  The warps' softmaxes are joined through shared memory, ranges by a second launch.
 constexpr int RW = 4;             // warps
 constexpr int RING = 3;
+constexpr float MOST = 65536.f;   // weights of a step that add up to more ask for a new reference
 template <int D>
 struct RowsShape {
   static constexpr int KEYS = 2048 / D;                   // of a step: 32 or 16
@@ -43,7 +44,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_constant__ Params P) {
   constexpr int R = 8 * NT, KEYS = RowsShape<D>::KEYS, STEP = RowsShape<D>::STEP_BYTES, PIECES = D / 8, AT_ONCE = 32 / PIECES, G16 = KEYS / 16;
-  constexpr uint32_t NOWHERE = 0xffffffffu;
   extern __shared__ unsigned char smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane & 3, mrow = lane >> 2;
   mst_grid_launch_dependents();
@@ -58,12 +58,13 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
     if (!locate(T, P, b, tile, R)) return;
     uint32_t lo, hi;
     int active;
-    if (!T.range(P.splits, P.least, UNIT, split, lo, hi, active)) continue;
+    if (!T.range(P.splits, P.by_least, split, lo, hi, active)) continue;
     const uint32_t total = (hi - lo + KEYS - 1) / KEYS;                                // steps of the block
     const uint32_t mine = total > (uint32_t)warp ? (total - warp + RW - 1) / RW : 0u;
     // Step s of this warp: entries lo + (s RW + warp) KEYS ..; places in the cache are numbers of 16-byte pieces.
-    // An entry's page is asked for a step before its number is used: the use would wait for the answer where it stands.
+    // An entry's page is asked for RING steps before its number is used: a warp stands still where it uses what has not come.
     Key keys[RING];
+    bool seen[RING];                  // every row sees every entry of the step
     struct Entry { Key key; int slot, id; };
     const uint32_t head_at = (uint32_t)((int64_t)kvh * P.C.head_stride / 8), page_step = (uint32_t)(P.C.page_stride / 8), slot_step = (uint32_t)(P.C.token_stride / 8);
     const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
@@ -77,40 +78,51 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
       }
       return e;
     };
+    // Addresses that a lane comes back to; what else there is to them (slot, sixteen, row) is a constant of the unrolled loop.  Swizzle: 16-byte
+    // piece p of row r at p ^ (r & 7).
+    const int c = lane % PIECES, r_in = lane / PIECES;
+    constexpr int SAME = 8 / AT_ONCE;       // copies whose rows take turns in the swizzle
+    uint32_t to[SAME];
+#pragma unroll
+    for (int i = 0; i < SAME; ++i) to[i] = piece<D>(ring, i * AT_ONCE + r_in, c);
+    const __nv_bfloat16 *from_k = P.C.K + c * 8, *from_v = P.C.V + c * 8;
+    uint32_t frag_k[D / 16], frag_v[D / 16];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      frag_k[k] = piece<D>(ring, lane & 15, k * 2 + (lane >> 4));
+      frag_v[k] = piece<D>(ring + STEP, (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1));
+    }
     auto load = [&](int slot, Entry e) {
-      uint32_t at = NOWHERE;
-      if (e.key.pos >= 0) {
-        if ((uint32_t)e.id < (uint32_t)P.C.num_pages) {
-          at = (uint32_t)e.id * page_step + (uint32_t)e.slot * slot_step + head_at;
-        } else {
-          e.key.pos = -1;
-          g_bad_page = 1;
-        }
+      const bool there = e.key.pos >= 0 && (uint32_t)e.id < (uint32_t)P.C.num_pages;
+      if (e.key.pos >= 0 && !there) {
+        e.key.pos = -1;
+        g_bad_page = 1;
       }
+      const uint32_t at = there ? (uint32_t)e.id * page_step + (uint32_t)e.slot * slot_step + head_at : 0u;
+      const uint32_t bits = __ballot_sync(0xffffffffu, there) >> r_in;
       keys[slot] = e.key;
-      const int c = lane % PIECES;
-      const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
+      seen[slot] = __all_sync(0xffffffffu, e.key.pos >= 0 && (e.key.who >= 0 ? T.nt == 1 : e.key.pos <= T.p_lo && T.p_hi - e.key.pos < T.l));
 #pragma unroll
       for (int r0 = 0; r0 < KEYS; r0 += AT_ONCE) {
-        const int r = r0 + lane / PIECES;
-        const uint32_t a = __shfl_sync(0xffffffffu, at, r);
-        const bool there = a != NOWHERE;
-        const int64_t from = (int64_t)(there ? a + (uint32_t)c : 0u) * 8;
-        cp16(piece<D>(kt, r, c), P.C.K + from, there);
-        cp16(piece<D>(vt, r, c), P.C.V + from, there);
+        const uint32_t a = __shfl_sync(0xffffffffu, at, r0 + r_in);
+        const uint32_t size = ((bits >> r0) & 1u) << 4;
+        const uint32_t dst = to[(r0 / AT_ONCE) % SAME] + (uint32_t)(slot * 2 * STEP + r0 / 8 * 8 * D * 2);
+        cp16_of(dst, from_k + (uint64_t)a * 8, size);
+        cp16_of(dst + STEP, from_v + (uint64_t)a * 8, size);
       }
     };
-    Entry next;
+    Entry ahead[RING];                // of the steps to be loaded next
     {
-      Entry ahead[RING];
+      Entry first[RING - 1];
 #pragma unroll
-      for (int s = 0; s < RING; ++s) ahead[s] = look((uint32_t)s);
+      for (int s = 0; s < RING - 1; ++s) first[s] = look((uint32_t)s);
+#pragma unroll
+      for (int s = RING - 1; s < 2 * RING - 1; ++s) ahead[s % RING] = look((uint32_t)s);
 #pragma unroll
       for (int s = 0; s < RING - 1; ++s) {
-        if ((uint32_t)s < mine) load(s, ahead[s]);
+        if ((uint32_t)s < mine) load(s, first[s]);
         cp_commit();
       }
-      next = ahead[RING - 1];
     }
     // queries: the right operand's published layout (column lane / 4, rows 2 (lane % 4) and + 8)
     uint32_t q[NT][D / 16][2];
@@ -148,12 +160,11 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
         cp_wait<RING - 2>();
         __syncwarp();                      // every lane's copies are in, and the slot to be filled has been read by every lane
         if (s + RING - 1 < mine) {
-          load((slot + RING - 1) % RING, next);
-          next = look(s + RING);
+          load((slot + RING - 1) % RING, ahead[(slot + RING - 1) % RING]);
+          ahead[(slot + RING - 1) % RING] = look(s + 2 * RING - 1);
         }
         cp_commit();
-        const uint32_t kt = ring + (uint32_t)(slot * 2 * STEP), vt = kt + STEP;
-        float x[NT][G16][4];               // keys lane / 4 and + 8 of each sixteen, rows 2 (lane % 4) and the next
+        float x[NT][G16][4], p[NT][G16][4];      // scores and weights: keys lane / 4 and + 8 of each sixteen, rows 2 (lane % 4) and the next
 #pragma unroll
         for (int g = 0; g < G16; ++g) {
 #pragma unroll
@@ -161,14 +172,13 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             uint32_t f[4];
-            ldsm_x4(f, piece<D>(kt, g * 16 + (lane & 15), k * 2 + (lane >> 4)));
+            ldsm_x4(f, frag_k[k] + (uint32_t)(slot * 2 * STEP + g * 16 * D * 2));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma_bf16(x[nt][g], f, q[nt][k][0], q[nt][k][1]);
           }
         }
         const Key key = keys[slot];
-        const bool all = key.pos >= 0 && (key.who >= 0 ? T.nt == 1 : key.pos <= T.p_lo && T.p_hi - key.pos < T.l);
-        if (!__all_sync(0xffffffffu, all)) {
+        if (!seen[slot]) {
 #pragma unroll
           for (int g = 0; g < G16; ++g)
 #pragma unroll
@@ -184,21 +194,35 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float top[2] = {-INFINITY, -INFINITY};
+          // Weights against the reference as it is.  Their sums tell whether a score lies too far above it, which is seldom: nobody waits for a maximum
+          float add[2];
+          auto weigh = [&]() {
+            const float r0 = reference(m[nt][0]), r1 = reference(m[nt][1]);
+            add[0] = add[1] = 0.f;
 #pragma unroll
-          for (int g = 0; g < G16; ++g)
+            for (int g = 0; g < G16; ++g) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) top[u] = fmaxf(top[u], fmaxf(x[nt][g][u], x[nt][g][2 + u]));
-          top[0] *= P.scale_log2;
-          top[1] *= P.scale_log2;
-          if (__any_sync(0xffffffffu, top[0] > m[nt][0] + LAZY || top[1] > m[nt][1] + LAZY)) {
+              for (int e = 0; e < 2; ++e) {
+                p[nt][g][2 * e] = ex2(fmaf(x[nt][g][2 * e], P.scale_log2, -r0));
+                p[nt][g][2 * e + 1] = ex2(fmaf(x[nt][g][2 * e + 1], P.scale_log2, -r1));
+              }
+              add[0] += p[nt][g][0] + p[nt][g][2];
+              add[1] += p[nt][g][1] + p[nt][g][3];
+            }
+          };
+          weigh();
+          if (__any_sync(0xffffffffu, add[0] > MOST || add[1] > MOST || m[nt][0] == -INFINITY || m[nt][1] == -INFINITY)) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
+              float top = -INFINITY;
 #pragma unroll
-              for (int d = 4; d < 32; d *= 2) top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], d));
-              const bool up = top[u] > m[nt][u] + LAZY;
-              const float c = up ? ex2(m[nt][u] - top[u]) : 1.f;
-              if (up) m[nt][u] = top[u];
+              for (int g = 0; g < G16; ++g) top = fmaxf(top, fmaxf(x[nt][g][u], x[nt][g][2 + u]));
+              top *= P.scale_log2;
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+              const bool up = top > m[nt][u];            // the same in all lanes of a row
+              const float c = up ? ex2(m[nt][u] - top) : 1.f;
+              if (up) m[nt][u] = top;
               sum[nt][u] *= c;
 #pragma unroll
               for (int d = 0; d < D / 16; ++d) {
@@ -206,31 +230,23 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
                 acc[nt][d][2 + u] *= c;
               }
             }
+            weigh();
           }
-          const float r0 = reference(m[nt][0]), r1 = reference(m[nt][1]);
-#pragma unroll
-          for (int g = 0; g < G16; ++g) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              x[nt][g][2 * e] = ex2(fmaf(x[nt][g][2 * e], P.scale_log2, -r0));
-              x[nt][g][2 * e + 1] = ex2(fmaf(x[nt][g][2 * e + 1], P.scale_log2, -r1));
-            }
-            sum[nt][0] += x[nt][g][0] + x[nt][g][2];
-            sum[nt][1] += x[nt][g][1] + x[nt][g][3];
-          }
+          sum[nt][0] += add[0];
+          sum[nt][1] += add[1];
         }
 #pragma unroll
         for (int g = 0; g < G16; ++g) {
           uint32_t w[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            w[nt][0] = transposed(pack_bf16(x[nt][g][0], x[nt][g][1]));
-            w[nt][1] = transposed(pack_bf16(x[nt][g][2], x[nt][g][3]));
+            w[nt][0] = transposed(pack_bf16(p[nt][g][0], p[nt][g][1]));
+            w[nt][1] = transposed(pack_bf16(p[nt][g][2], p[nt][g][3]));
           }
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) {
             uint32_t f[4];
-            ldsm_x4_t(f, piece<D>(vt, g * 16 + (lane & 7) + (lane >> 4) * 8, d * 2 + ((lane >> 3) & 1)));
+            ldsm_x4_t(f, frag_v[d] + (uint32_t)(slot * 2 * STEP + g * 16 * D * 2));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][d], f, w[nt][0], w[nt][1]);
           }
@@ -322,7 +338,7 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
     TileWalk(T, (int64_t)P.B.table_stride * P.C.page_size).range(P.splits, P.least, 0, n0, n1, m0, m1, active);
   } else {
     uint32_t lo, hi;
-    T.range(P.splits, P.least, UNIT, 0, lo, hi, active);
+    T.range(P.splits, P.by_least, 0, lo, hi, active);
   }
   if (active == 1) return;
   // lane s: ranges s and s + 32 (there are 64 at most)
@@ -388,7 +404,7 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
     units = (list + UNIT - 1) / UNIT;
     p.least = 8;
   }
-  const int64_t blocks = lists * tiles, want = (p.tiles ? 8 : 12) * (int64_t)mst_sm_count();
+  const int64_t blocks = lists * tiles, want = (p.tiles ? 8 : 4) * (int64_t)mst_sm_count();
   int64_t splits = (want + blocks - 1) / blocks;
   const int64_t fit = (units + p.least - 1) / p.least;
   if (splits > fit) splits = fit;
@@ -487,6 +503,8 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   P.scale_log2 = LOG2E / sqrtf((float)cache->head_dim);
   P.splits = plan.splits;
   P.least = plan.least;
+  P.by_l = Divider::of((uint32_t)stride);
+  P.by_least = Divider::of((uint32_t)plan.least);
   P.part_o = (float*)workspace;
   if (need) P.part_m = P.part_o + (size_t)plan.splits * (size_t)batch->tokens * (size_t)heads * (size_t)cache->head_dim;
   cudaStream_t s = (cudaStream_t)stream;

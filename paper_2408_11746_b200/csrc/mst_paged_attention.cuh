@@ -23,7 +23,7 @@ struct Params {
   float* lse;
   int64_t ldq, ldo;
   int heads, group, l;
-  Divider by_group;
+  Divider by_group, by_l, by_least;
   float scale_log2;
   int splits, least;      // most ranges of a list, and the least units of one (plan)
   float* part_o;          // [splits][tokens * heads][D]: sums against part_m, [splits][tokens * heads][2]: reference and sum of weights
@@ -36,14 +36,16 @@ constexpr int UNIT = 64;  // keys of a list that stay together
 __device__ __forceinline__ bool locate(List& T, const Params& P, int b, int tile, int R) {
   const int len = P.B.len[b];
   const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.by_group, P.l, reach, tile, R)) return false;
+  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.by_group, P.by_l, reach, tile, R)) return false;
   if (len > reach) g_bad_page = 1;
   return true;
 }
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// 16 bytes, of which `size` (16 or none) come from src, which lies in the cache either way, and the others are zero
+__device__ __forceinline__ void cp16_of(uint32_t dst, const void* src, uint32_t size) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
 }
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) { cp16_of(dst, src, there ? 16u : 0u); }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {

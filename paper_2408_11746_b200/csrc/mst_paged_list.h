@@ -51,9 +51,9 @@ struct List {
 
   // Tile `tile` of `R` pairs of a sequence with rows first .. end - 1 of `tokens` and `len` positions, `group` query heads to a key head, `reach`
   // positions that its table has room for.  false: no such tile.
-  MST_HD bool locate(int first_, int end, int len, int tokens, const Divider& group, int stride, int64_t reach, int tile, int R) {
+  MST_HD bool locate(int first_, int end, int len, int tokens, const Divider& group, const Divider& stride, int64_t reach, int tile, int R) {
     first = first_;
-    l = stride;
+    l = (int)stride.d;
     if (first < 0 || end <= first || end > tokens) return false;
     const int n = end - first;
     const int64_t all = (int64_t)n * group.d, r0 = (int64_t)tile * R;
@@ -70,7 +70,7 @@ struct List {
     const int64_t w = dense ? 0 : (int64_t)p_lo - l + 1;
     w0 = w > 0 ? (int)w : 0;
     W = last >= w0 ? (uint32_t)(last - w0 + 1) : 0u;
-    N = W + (dense || p_hi < l ? 0u : (uint32_t)(p_hi / l) * (uint32_t)nt);
+    N = W + (dense || p_hi < l ? 0u : (uint32_t)stride.over(p_hi) * (uint32_t)nt);
     return true;
   }
   MST_HD Key key(uint32_t n) const {
@@ -93,14 +93,21 @@ struct List {
     const int back = p - k.pos;       // both within 2^31 of each other: positions from -2^30 on
     return back >= 0 && (back < l || (dense && back % l == 0));
   }
-  // Range `split` of at most `splits` ranges of whole units of `unit` entries, `least` of them at least.  active: how many ranges there are.
-  MST_HD bool range(int splits, int least, int unit, int split, uint32_t& lo, uint32_t& hi, int& active) const {
-    const uint32_t units = N / (uint32_t)unit + (N % (uint32_t)unit != 0 ? 1u : 0u);
-    uint32_t each = units / (uint32_t)splits + (units % (uint32_t)splits != 0 ? 1u : 0u);
-    if (each < (uint32_t)least) each = (uint32_t)least;
-    active = units == 0 ? 1 : (int)(units / each + (units % each != 0 ? 1u : 0u));
+  // Range `split` of at most `splits` ranges of whole units of 64 entries, `least` of them at least.  active: how many ranges there are.
+  MST_HD bool range(int splits, const Divider& least, int split, uint32_t& lo, uint32_t& hi, int& active) const {
+    const uint32_t units = N / 64 + (N % 64 != 0 ? 1u : 0u);
+    uint32_t each = least.d;
+    if (splits == 1) {
+      each = units;
+      active = 1;
+    } else if (units <= (uint64_t)each * (uint32_t)splits) {
+      active = units == 0 ? 1 : least.over((int)(units - 1)) + 1;
+    } else {           // longer than the launch was told
+      each = units / (uint32_t)splits + (units % (uint32_t)splits != 0 ? 1u : 0u);
+      active = (int)(units / each + (units % each != 0 ? 1u : 0u));
+    }
     if (split >= active) return false;
-    const uint64_t a = (uint64_t)each * (uint32_t)split * (uint32_t)unit, z = a + (uint64_t)each * (uint32_t)unit;
+    const uint64_t a = (uint64_t)each * (uint32_t)split * 64u, z = a + (uint64_t)each * 64u;
     lo = (uint32_t)a;
     hi = z < N ? (uint32_t)z : N;
     return true;

@@ -88,6 +88,8 @@ __global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid
       int head;
       const int side = side_of(i, head);
       Raw<T> out = raw[u];
+      const Raw<T> in = raw[u];
+      if (i + AHEAD < end) fetch(i + AHEAD, raw[u]);
       if (!APPEND || side < 2) {
         if (side != cur) {
           const float* gamma = side == 0 ? P.R.gamma_q : P.R.gamma_k;
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid
           }
           cur = side;
         }
-        const Pairs x = widen<INTER>(raw[u]);
+        const Pairs x = widen<INTER>(in);
         Pairs y;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -132,10 +134,6 @@ __global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid
         else if (!APPEND) store_row(out, out_k + head * P.R.D, L);
         else if (slot.exists) store_row(out, (side == 1 ? out_k : out_v) + head * P.cache.head_stride, L);
       }
-    }
-    if (i0 + AHEAD < end) {
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) fetch(i0 + AHEAD + u, raw[u]);
     }
   }
 }

@@ -10,19 +10,19 @@ extern "C" {
 // info: row0, rows, t_lo, nt, p_lo, p_hi, W, N, dense; 0 where there is no such tile
 int list_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int64_t* info) {
   List T;
-  if (!T.locate(first, end, len, tokens, Divider::of(group), stride, reach, tile, R)) return 0;
+  if (!T.locate(first, end, len, tokens, Divider::of(group), Divider::of(stride), reach, tile, R)) return 0;
   const int64_t v[9] = {T.row0, T.rows, T.t_lo, T.nt, T.p_lo, T.p_hi, (int64_t)T.W, (int64_t)T.N, T.dense};
   for (int i = 0; i < 9; ++i) info[i] = v[i];
   return 1;
 }
 
-int range_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int splits, int least, int unit,
+int range_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int splits, int least,
              int split, int64_t* lo_hi_active) {
   List T;
-  if (!T.locate(first, end, len, tokens, Divider::of(group), stride, reach, tile, R)) return -1;
+  if (!T.locate(first, end, len, tokens, Divider::of(group), Divider::of(stride), reach, tile, R)) return -1;
   uint32_t lo = 0, hi = 0;
   int active = 0;
-  const int there = T.range(splits, least, unit, split, lo, hi, active);
+  const int there = T.range(splits, Divider::of(least), split, lo, hi, active);
   lo_hi_active[0] = lo;
   lo_hi_active[1] = hi;
   lo_hi_active[2] = active;
@@ -33,7 +33,7 @@ int range_of(int first, int end, int len, int tokens, int group, int stride, int
 int keys_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int64_t lo, int64_t hi, int32_t* pos,
             int32_t* who, uint8_t* seen) {
   List T;
-  if (!T.locate(first, end, len, tokens, Divider::of(group), stride, reach, tile, R)) return 0;
+  if (!T.locate(first, end, len, tokens, Divider::of(group), Divider::of(stride), reach, tile, R)) return 0;
   for (int64_t n = lo; n < hi; ++n) {
     const Key k = T.key((uint32_t)n);
     pos[n - lo] = k.pos;
@@ -47,7 +47,7 @@ int keys_of(int first, int end, int len, int tokens, int group, int stride, int6
 int walk_of(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int splits, int least, int split,
             int32_t* out) {
   List T;
-  if (!T.locate(first, end, len, tokens, Divider::of(group), stride, reach, tile, R)) return -1;
+  if (!T.locate(first, end, len, tokens, Divider::of(group), Divider::of(stride), reach, tile, R)) return -1;
   const mst_paged::TileWalk w(T, reach);
   int r[5] = {};
   const int there = w.range(splits, least, split, r[0], r[1], r[2], r[3], r[4]);
@@ -57,7 +57,7 @@ int walk_of(int first, int end, int len, int tokens, int group, int stride, int6
 }
 int near(int first, int end, int len, int tokens, int group, int stride, int64_t reach, int tile, int R, int p, int k) {
   List T;
-  if (!T.locate(first, end, len, tokens, Divider::of(group), stride, reach, tile, R)) return -1;
+  if (!T.locate(first, end, len, tokens, Divider::of(group), Divider::of(stride), reach, tile, R)) return -1;
   return mst_paged::near_sees(T.l, p, k);
 }
 

@@ -30,7 +30,7 @@ def _tile(lib, args):
     return list(info) if lib.list_of(*args, info) else None
 
 
-def _seen_by_rows(lib, n, length, group, stride, R, splits, least, unit, reach=BIG):
+def _seen_by_rows(lib, n, length, group, stride, R, splits, least, reach=BIG):
     """{row of the sequence: positions it looks at, in list order over all ranges}"""
     out, tile = {}, 0
     while True:
@@ -44,12 +44,12 @@ def _seen_by_rows(lib, n, length, group, stride, R, splits, least, unit, reach=B
         end, split = 0, 0
         while True:
             lha = (ctypes.c_int64 * 3)()
-            there = lib.range_of(*args, splits, least, unit, split, lha)
+            there = lib.range_of(*args, splits, least, split, lha)
             if not there:
                 break
             lo, hi, active = list(lha)
             assert lo == end and hi >= lo and (hi > lo or N == 0) and split < active <= splits
-            assert lo % unit == 0
+            assert lo % 64 == 0
             end = hi
             pos, who = np.empty(hi - lo, np.int32), np.empty(hi - lo, np.int32)
             got = np.empty((hi - lo, nt), np.uint8)
@@ -67,7 +67,8 @@ def _seen_by_rows(lib, n, length, group, stride, R, splits, least, unit, reach=B
 @pytest.mark.parametrize("n,length,group,R", [(1, 1, 1, 16), (1, 700, 1, 16), (1, 129, 5, 16), (5, 300, 2, 16), (7, 7, 3, 16), (40, 333, 1, 32),
                                               (9, 200, 40, 32), (130, 400, 1, 128), (70, 500, 4, 128), (3, 2, 2, 16), (4, 0, 1, 16)])
 def test_rows_look_at_their_sets(lib, n, length, group, R, stride):
-    got = _seen_by_rows(lib, n, length, group, stride, R, splits=3, least=2, unit=16)
+    got = _seen_by_rows(lib, n, length, group, stride, R, splits=3, least=1)
+    assert got == _seen_by_rows(lib, n, length, group, stride, R, splits=1, least=4)
     assert sorted(got) == list(range(n * group))
     for r, seen in got.items():
         i = length - n + r // group
@@ -121,7 +122,7 @@ def test_tiles_of_lengths_that_make_no_sense(lib, length, stride, reach):
 
 
 def test_rows_stay_within_the_table(lib):
-    got = _seen_by_rows(lib, 4, 100, 1, 64, 16, 2, 1, 16, reach=80)
+    got = _seen_by_rows(lib, 4, 100, 1, 64, 16, 2, 1, reach=80)
     for r, seen in got.items():
         i = 96 + r
         assert set(seen) >= {j for j in range(80) if 0 <= i - j < 64}
@@ -143,7 +144,7 @@ def test_lengths_that_make_no_sense(lib, length, stride, reach):
     if length <= 0:
         assert N == 0
     lha = (ctypes.c_int64 * 3)()
-    assert lib.range_of(*args, 64, 4, 64, 0, lha) == 1
+    assert lib.range_of(*args, 64, 4, 0, lha) == 1
     for n in {0, W // 2, max(W - 1, 0), W, min(W + 1, max(N - 1, 0)), max(N - 1, 0), N}:
         pos, who, got = np.empty(1, np.int32), np.empty(1, np.int32), np.empty((1, nt), np.uint8)
         lib.keys_of(*args, ctypes.c_int64(n), ctypes.c_int64(n + 1), pos.ctypes, who.ctypes, got.ctypes)
