@@ -2,7 +2,7 @@
 // appends to a paged cache.  The arithmetic of a row is in mst_rotate.cuh; the kernels differ in where rows come from and go to.
 //
 // Bound: HBM (each row is read once and written once), or a launch and a trip to memory where there are few tokens.  A warp takes a token (or
-// a share of its heads) and has the loads of four steps in flight before it works out the angles; no block-wide step anywhere.
+// a share of its heads) and has the loads of its first steps in flight before it works out the angles; no block-wide step on the way.
 #include "mst_paged.cuh"
 #include "mst_rotate.cuh"
 
@@ -20,47 +20,41 @@ struct RowsParams {
   const int32_t* positions;
   int seq_len;
   int tokens;
-  int per_warp;                // steps of a warp
+  int groups_q, steps;         // groups of lanes that take queries, steps of a token's queries and keys
+  int per_warp;                // steps of a warp, those of the values (appending) among them
   mst_paged::Cache cache;
   mst_paged::Batch batch;
 };
 
-constexpr int AHEAD = 4;       // steps whose loads are in flight together
-
 template <typename T, int G, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid_constant__ RowsParams P) {
+__global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid_constant__ RowsParams P) {
+  constexpr int AHEAD = sizeof(T) == 2 ? 3 : 2;      // steps whose loads are in flight together
+  constexpr int ALL = 32 / G;
   __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
-  constexpr int ROWS = 32 / G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
   const unsigned at = blockIdx.x * WARPS + warp;
   if (at >= (unsigned)P.tokens) return;
   const int token = (int)at;
-  const Steps steps(ROWS, P.hq, P.hk, APPEND ? P.hk : 0);
-  const int begin = (int)blockIdx.y * P.per_warp;
-  const int end = begin + P.per_warp < steps.all() ? begin + P.per_warp : steps.all();
+  const int begin = (int)blockIdx.y * P.per_warp, all_end = begin + P.per_warp;
+  const int end = all_end < P.steps ? all_end : P.steps;
   const Lane L(P.R, lane % G, INTER);
-  const int row = lane / G;
-  const int64_t jump = (int64_t)row * P.R.D;                                    // this lane's row of a step
-  const T* in_q = (const T*)P.Q + token * P.ld + jump;
-  const T* in_k = (const T*)P.K + token * P.ld + jump;
-  const T* in_v = APPEND ? (const T*)P.V + token * P.ld + jump : nullptr;
-  // side of a step, its rows' first head
-  auto side_of = [&](int i, int& head) {
-    const int side = i < steps.q ? 0 : !APPEND || i < steps.q + steps.k ? 1 : 2;
-    head = (side == 0 ? i : side == 1 ? i - steps.q : i - steps.q - steps.k) * ROWS;
-    return side;
-  };
-  auto fetch = [&](int i, Raw<T>& r) {
-    int head;
-    const int side = side_of(i, head);
-    no_row(r);
-    if (i < end && L.in && head + row < (side == 0 ? P.hq : P.hk)) load_row(r, (side == 0 ? in_q : side == 1 ? in_k : in_v) + head * P.R.D, L);
-  };
+  // this lane's side: its group's first head and how far apart its heads are
+  const int group = lane / G;
+  const bool is_q = group < P.groups_q;
+  const int head0 = is_q ? group : group - P.groups_q, every = is_q ? P.groups_q : ALL - P.groups_q, heads = is_q ? P.hq : P.hk;
+  const T* in = (const T*)(is_q ? P.Q : P.K) + token * P.ld + (int64_t)head0 * P.R.D;
+  const int in_step = every * P.R.D;
+  auto mine = [&](int i) { return i < end && L.in && head0 + i * every < heads; };
   Raw<T> raw[AHEAD];
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) fetch(begin + u, raw[u]);
+  for (int u = 0; u < AHEAD; ++u) {
+    no_row(raw[u]);
+    if (mine(begin + u)) load_row(raw[u], in + (int64_t)(begin + u) * in_step, L);
+  }
+  const float* gamma = is_q ? P.R.gamma_q : P.R.gamma_k;
+  const Pairs g = weights<INTER>(gamma, L);
   int pos;
   mst_paged::Slot slot = {true, 0};
   if (APPEND) {
@@ -72,67 +66,71 @@ __global__ void __launch_bounds__(32 * WARPS, 3) rotate_rows_kernel(const __grid
   } else {
     pos = P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len);
   }
-  T* out_q = (T*)P.Qo + token * P.ldq + jump;
-  T* out_k = APPEND ? (T*)P.cache.K + slot.at + row * P.cache.head_stride : (T*)P.Ko + token * P.ldq + jump;
-  T* out_v = APPEND ? (T*)P.cache.V + slot.at + row * P.cache.head_stride : nullptr;
-  const Turn turn = turn_of<INTER>(tables[warp], P.R, L, pos, lane);
-  const float inv_d = 1.f / (float)P.R.D;
-  Pairs A = {}, B = {};      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
-  bool norm = false;
-  int cur = -1;
-  for (int i0 = begin; i0 < end; i0 += AHEAD) {
+  if (begin < P.steps) {
+    const bool to_cache = APPEND && !is_q;
+    T* out = to_cache ? (T*)P.cache.K + slot.at + head0 * P.cache.head_stride
+                      : (T*)(is_q ? P.Qo : P.Ko) + token * P.ldq + (int64_t)head0 * P.R.D;
+    const int64_t out_step = to_cache ? every * P.cache.head_stride : (int64_t)in_step;
+    const bool writes = !to_cache || slot.exists;
+    Pairs A, B;      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
+    {
+      const Turn turn = turn_of<INTER>(tables[warp], P.R, L, pos, lane);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int i = i0 + u;
-      if (i >= end) break;
-      int head;
-      const int side = side_of(i, head);
-      Raw<T> out = raw[u];
-      const Raw<T> in = raw[u];
-      if (i + AHEAD < end) fetch(i + AHEAD, raw[u]);
-      if (!APPEND || side < 2) {
-        if (side != cur) {
-          const float* gamma = side == 0 ? P.R.gamma_q : P.R.gamma_k;
-          norm = gamma != nullptr;
-          const Pairs g = weights<INTER>(gamma, L);
+      for (int k = 0; k < 4; ++k) {
+        A.u[k] = mul2(g.u[k], turn.c[k]);
+        A.v[k] = mul2(g.u[k], turn.s[k]);
+        B.u[k] = negated(mul2(g.v[k], turn.s[k]));
+        B.v[k] = mul2(g.v[k], turn.c[k]);
+      }
+    }
+    const float inv_d = 1.f / (float)P.R.D;
+    const bool norm = gamma != nullptr, alone = !L.turns;      // alone: no pairs, an infinite value stays on its own
+    for (int i0 = begin; i0 < end; i0 += AHEAD) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            A.u[k] = mul2(g.u[k], turn.c[k]);
-            A.v[k] = mul2(g.u[k], turn.s[k]);
-            B.u[k] = negated(mul2(g.v[k], turn.s[k]));
-            B.v[k] = mul2(g.v[k], turn.c[k]);
-          }
-          cur = side;
-        }
-        const Pairs x = widen<INTER>(in);
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u;
+        if (i >= end) break;
+        const Pairs x = widen<INTER>(raw[u]);
+        if (mine(i + AHEAD)) load_row(raw[u], in + (int64_t)(i + AHEAD) * in_step, L);
         Pairs y;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          y.u[k] = fma2(x.v[k], B.u[k], mul2(x.u[k], A.u[k]));
-          y.v[k] = fma2(x.v[k], B.v[k], mul2(x.u[k], A.v[k]));
+        for (int k = 0; k < 4; ++k) {
+          y.u[k] = mul2(x.u[k], A.u[k]);
+          y.v[k] = mul2(x.v[k], B.v[k]);
         }
-        if (P.R.rot < P.R.D && !L.turns) {     // no pairs: an infinite value stays on its own
+        if (!alone) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            y.u[k] = mul2(x.u[k], A.u[k]);
-            y.v[k] = mul2(x.v[k], B.v[k]);
+          for (int k = 0; k < 4; ++k) {
+            y.u[k] = fma2(x.v[k], B.u[k], y.u[k]);
+            y.v[k] = fma2(x.u[k], A.v[k], y.v[k]);
           }
         }
-        if (norm) {
-          const float r = rsqrtf(fmaf(sum_lanes<G>(dot(x, x)), inv_d, P.R.eps));
-          const uint64_t r2 = pack2(r, r);
+        const float sum = sum_lanes<G>(dot(x, x));       // every lane: it has shuffles
+        const float r = norm ? rsqrtf(fmaf(sum, inv_d, P.R.eps)) : 1.f;
+        const uint64_t r2 = pack2(r, r);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            y.u[k] = mul2(y.u[k], r2);
-            y.v[k] = mul2(y.v[k], r2);
-          }
+        for (int k = 0; k < 4; ++k) {
+          y.u[k] = mul2(y.u[k], r2);
+          y.v[k] = mul2(y.v[k], r2);
         }
-        narrow<INTER>(y, out);
+        if (mine(i) && writes) {
+          Raw<T> o;
+          narrow<INTER>(y, o);
+          store_row(o, out + i * out_step, L);
+        }
       }
-      if (L.in && head + row < (side == 0 ? P.hq : P.hk)) {
-        if (side == 0) store_row(out, out_q + head * P.R.D, L);
-        else if (!APPEND) store_row(out, out_k + head * P.R.D, L);
-        else if (slot.exists) store_row(out, (side == 1 ? out_k : out_v) + head * P.cache.head_stride, L);
+    }
+  }
+  if (APPEND && slot.exists) {      // the values are carried over as they are
+    const int v0 = begin > P.steps ? begin - P.steps : 0, v1 = all_end - P.steps;
+    const T* from = (const T*)P.V + token * P.ld;
+    T* to = (T*)P.cache.V + slot.at;
+    for (int i = v0; i < v1; ++i) {
+      const int head = i * ALL + group;
+      if (head < P.hk && L.in) {
+        Raw<T> r;
+        load_row(r, from + (int64_t)head * P.R.D, L);
+        store_row(r, to + head * P.cache.head_stride, L);
       }
     }
   }
@@ -148,126 +146,125 @@ struct GradParams {
   const int32_t* positions;
   int seq_len;
   int tokens;
-  int share, per_warp;
+  int groups_q, steps, share, per_warp;
   float* partial;        // [blocks][2][D]: sums of the weights' gradients, or NULL
 };
 
 // Blocks that stay: each warp goes on to the token that lies a grid further, with its share of the weights' gradients in registers, so that a
 // block leaves 2 D sums in all.
-constexpr int GRAD_BLOCKS_PER_SM = 2, GRAD_AHEAD = 2;
+constexpr int GRAD_BLOCKS_PER_SM = 2;
 constexpr int GRAD_BLOCKS_MOST = 512;
 
 template <typename T, int G, bool INTER>
 __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_kernel(const __grid_constant__ GradParams P) {
+  constexpr int ALL = 32 / G;
   __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
-  constexpr int ROWS = 32 / G;
+  __shared__ float sums[WARPS][2][256];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
-  const Steps steps(ROWS, P.hq, P.hk, 0);
   const Lane L(P.R, lane % G, INTER);
-  const int row = lane / G;
-  const int64_t jump = (int64_t)row * P.R.D;
+  const int group = lane / G;
+  const bool is_q = group < P.groups_q;
+  const int head0 = is_q ? group : group - P.groups_q, every = is_q ? P.groups_q : ALL - P.groups_q, heads = is_q ? P.hq : P.hk;
+  const int step = every * P.R.D;
+  const float* gamma = is_q ? P.R.gamma_q : P.R.gamma_k;
+  const bool norm = gamma != nullptr, alone = !L.turns;
   const float inv_d = 1.f / (float)P.R.D;
-  const Pairs gq = weights<INTER>(P.R.gamma_q, L), gk = weights<INTER>(P.R.gamma_k, L);
-  Pairs acc_q = {}, acc_k = {};
+  const Pairs g = weights<INTER>(gamma, L);
+  Pairs acc = {};
   const unsigned groups = ((unsigned)P.tokens + WARPS - 1) / WARPS, all = groups * (unsigned)P.share;
   for (unsigned unit = blockIdx.x; unit < all; unit += gridDim.x) {
     const unsigned part = P.share > 1 ? unit / groups : 0u, at = (unit - part * groups) * WARPS + warp;
     if (at >= (unsigned)P.tokens) continue;
     const int token = (int)at;
     const int begin = (int)part * P.per_warp;
-    const int end = begin + P.per_warp < steps.all() ? begin + P.per_warp : steps.all();
-    const T *x_q = (const T*)P.Q + token * P.ld + jump, *x_k = (const T*)P.K + token * P.ld + jump;
-    const T *y_q = (const T*)P.dQo + token * P.lddo + jump, *y_k = (const T*)P.dKo + token * P.lddo + jump;
-    T *d_q = (T*)P.dQ + token * P.ldg + jump, *d_k = (T*)P.dK + token * P.ldg + jump;
-    Raw<T> rx[GRAD_AHEAD], ry[GRAD_AHEAD];
-    auto fetch = [&](int i, Raw<T>& x, Raw<T>& y) {
-      const bool q = i < steps.q;
-      const int head = (q ? i : i - steps.q) * ROWS;
-      no_row(x);
-      no_row(y);
-      if (i < end && L.in && head + row < (q ? P.hq : P.hk)) {
-        load_row(y, (q ? y_q : y_k) + head * P.R.D, L);
-        if (q ? P.R.gamma_q : P.R.gamma_k) load_row(x, (q ? x_q : x_k) + head * P.R.D, L);
+    const int end = begin + P.per_warp < P.steps ? begin + P.per_warp : P.steps;
+    const int64_t off = (int64_t)head0 * P.R.D;
+    const T* x_in = (const T*)(is_q ? P.Q : P.K) + token * P.ld + off;
+    const T* y_in = (const T*)(is_q ? P.dQo : P.dKo) + token * P.lddo + off;
+    T* out = (T*)(is_q ? P.dQ : P.dK) + token * P.ldg + off;
+    auto mine = [&](int i) { return i < end && L.in && head0 + i * every < heads; };
+    Raw<T> rx, ry;
+    auto fetch = [&](int i) {
+      if (mine(i)) {
+        load_row(ry, y_in + (int64_t)i * step, L);
+        if (norm) load_row(rx, x_in + (int64_t)i * step, L);
       }
     };
-#pragma unroll
-    for (int u = 0; u < GRAD_AHEAD; ++u) fetch(begin + u, rx[u], ry[u]);
+    no_row(rx);
+    no_row(ry);
+    fetch(begin);
     const Turn turn = turn_of<INTER>(tables[warp], P.R, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
-    for (int i0 = begin; i0 < end; i0 += GRAD_AHEAD) {
+    for (int i = begin; i < end; ++i) {
+      const bool here = mine(i);
+      const Pairs y = widen<INTER>(ry), x = widen<INTER>(rx);
+      fetch(i + 1);
+      Pairs z;
 #pragma unroll
-      for (int u = 0; u < GRAD_AHEAD; ++u) {
-        const int i = i0 + u;
-        if (i >= end) break;
-        const bool q = i < steps.q;
-        const int head = (q ? i : i - steps.q) * ROWS;
-        const Pairs y = widen<INTER>(ry[u]), x = widen<INTER>(rx[u]);
-        if (i + GRAD_AHEAD < end) fetch(i + GRAD_AHEAD, rx[u], ry[u]);
-        Pairs z;
+      for (int k = 0; k < 4; ++k) {
+        z.u[k] = mul2(y.u[k], turn.c[k]);
+        z.v[k] = mul2(y.v[k], turn.c[k]);
+      }
+      if (!alone) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          z.u[k] = fma2(y.v[k], turn.s[k], mul2(y.u[k], turn.c[k]));
-          z.v[k] = fma2(y.u[k], negated(turn.s[k]), mul2(y.v[k], turn.c[k]));
+        for (int k = 0; k < 4; ++k) {
+          z.u[k] = fma2(y.v[k], turn.s[k], z.u[k]);
+          z.v[k] = fma2(y.u[k], negated(turn.s[k]), z.v[k]);
         }
-        if (P.R.rot < P.R.D && !L.turns) z = y;
-        if (q ? P.R.gamma_q : P.R.gamma_k) {
-          Pairs g;        // z gamma
-          float r, back;
-          if (q) {
+      }
+      Pairs zg;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) { g.u[k] = mul2(z.u[k], gq.u[k]); g.v[k] = mul2(z.v[k], gq.v[k]); }
-          } else {
+      for (int k = 0; k < 4; ++k) {
+        zg.u[k] = mul2(z.u[k], g.u[k]);
+        zg.v[k] = mul2(z.v[k], g.v[k]);
+      }
+      const float sq = sum_lanes<G>(dot(x, x)), sd = sum_lanes<G>(dot(zg, x));     // every lane: they have shuffles
+      if (norm) {
+        const float r = rsqrtf(fmaf(sq, inv_d, P.R.eps)), back = -r * r * (sd * inv_d);
+        const uint64_t r2 = pack2(r, r), b2 = pack2(back, back);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) { g.u[k] = mul2(z.u[k], gk.u[k]); g.v[k] = mul2(z.v[k], gk.v[k]); }
+        for (int k = 0; k < 4; ++k) {
+          if (here) {       // rows that are not there may be another step's
+            acc.u[k] = fma2(z.u[k], mul2(x.u[k], r2), acc.u[k]);
+            acc.v[k] = fma2(z.v[k], mul2(x.v[k], r2), acc.v[k]);
           }
-          r = rsqrtf(fmaf(sum_lanes<G>(dot(x, x)), inv_d, P.R.eps));
-          back = -r * r * (sum_lanes<G>(dot(g, x)) * inv_d);
-          const uint64_t r2 = pack2(r, r), b2 = pack2(back, back);
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint64_t nu = mul2(x.u[k], r2), nv = mul2(x.v[k], r2);
-            if (q) {
-              acc_q.u[k] = fma2(z.u[k], nu, acc_q.u[k]);
-              acc_q.v[k] = fma2(z.v[k], nv, acc_q.v[k]);
-            } else {
-              acc_k.u[k] = fma2(z.u[k], nu, acc_k.u[k]);
-              acc_k.v[k] = fma2(z.v[k], nv, acc_k.v[k]);
-            }
-            z.u[k] = mul2(r2, fma2(b2, x.u[k], g.u[k]));
-            z.v[k] = mul2(r2, fma2(b2, x.v[k], g.v[k]));
-          }
+          z.u[k] = mul2(r2, fma2(b2, x.u[k], zg.u[k]));
+          z.v[k] = mul2(r2, fma2(b2, x.v[k], zg.v[k]));
         }
-        if (L.in && head + row < (q ? P.hq : P.hk)) {
-          Raw<T> out;
-          narrow<INTER>(z, out);
-          store_row(out, (q ? d_q : d_k) + head * P.R.D, L);
-        }
+      }
+      if (here) {
+        Raw<T> o;
+        narrow<INTER>(z, o);
+        store_row(o, out + (int64_t)i * step, L);
       }
     }
   }
   if (!P.partial) return;
-  // rows of a warp, then the warps, in a fixed order; the tables' place is free once every warp is here
-  float* sums = reinterpret_cast<float*>(tables);   // [WARPS][D]: 8 * 256 floats at most
-  static_assert(sizeof(tables) >= sizeof(float) * WARPS * 256, "a block's sums fit the tables");
+  // the groups of a warp, then the warps, in a fixed order
+  for (int e = threadIdx.x; e < WARPS * 2 * 256; e += 32 * WARPS) (&sums[0][0][0])[e] = 0.f;
+  __syncthreads();
+  float v[16];
+  values_of<INTER>(acc, v);
+  float* to = sums[warp][is_q ? 0 : 1];
+#pragma unroll 1
+  for (int k = 0; k < ALL; ++k) {
+    if (group == k && L.in) {
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    __syncthreads();
-    float v[8];
-    values_of<INTER>(side == 0 ? acc_q : acc_k, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-#pragma unroll
-      for (int o = G; o < 32; o *= 2) v[e] += __shfl_xor_sync(0xffffffffu, v[e], o);
-      if (lane < G && L.in) sums[warp * P.R.D + (e < 4 ? L.near + e : L.far + e - 4)] = v[e];
+      for (int e = 0; e < 8; ++e) {
+        to[L.near + e] += v[e];
+        if (L.in_far) to[L.far + e] += v[8 + e];
+      }
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < P.R.D; e += 32 * WARPS) {
-      float t = 0.f;
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < 2 * P.R.D; e += 32 * WARPS) {
+    const int side = e >= P.R.D, i = e - side * P.R.D;
+    float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < WARPS; ++k) t += sums[k * P.R.D + e];
-      P.partial[((int64_t)blockIdx.x * 2 + side) * P.R.D + e] = t;
-    }
+    for (int k = 0; k < WARPS; ++k) t += sums[k][side][i];
+    P.partial[((int64_t)blockIdx.x * 2 + side) * P.R.D + i] = t;
   }
 }
 
@@ -298,8 +295,10 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
 
 template <typename T, int G, bool INTER, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
-  const Steps steps(32 / G, P.hq, P.hk, APPEND ? P.hk : 0);
-  const int share = share_token(P.tokens, steps.all(), &P.per_warp);
+  const Groups g = groups_of(G, P.hq, P.hk);
+  P.groups_q = g.q;
+  P.steps = g.steps;
+  const int share = share_token(P.tokens, g.steps + (APPEND ? (P.hk + 32 / G - 1) / (32 / G) : 0), &P.per_warp);
   const unsigned blocks = ((unsigned)P.tokens + WARPS - 1) / WARPS;
   if (share > 65535) return MST_ERR_SHAPE;
   MST_CUDA_TRY(mst_launch_overlapped(rotate_rows_kernel<T, G, INTER, APPEND>, dim3(blocks, (unsigned)share), dim3(32 * WARPS), 0, s, P));
@@ -308,10 +307,10 @@ mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
 template <typename T, bool INTER, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
   switch (lanes_of(P.R.D)) {
+    case 2: return launch_rows<T, 2, INTER, APPEND>(P, s);
     case 4: return launch_rows<T, 4, INTER, APPEND>(P, s);
     case 8: return launch_rows<T, 8, INTER, APPEND>(P, s);
-    case 16: return launch_rows<T, 16, INTER, APPEND>(P, s);
-    default: return launch_rows<T, 32, INTER, APPEND>(P, s);
+    default: return launch_rows<T, 16, INTER, APPEND>(P, s);
   }
 }
 template <typename T, bool APPEND>
@@ -320,8 +319,10 @@ mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
 }
 template <typename T, int G, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
-  const Steps steps(32 / G, P.hq, P.hk, 0);
-  P.share = share_token(P.tokens, steps.all(), &P.per_warp);
+  const Groups g = groups_of(G, P.hq, P.hk);
+  P.groups_q = g.q;
+  P.steps = g.steps;
+  P.share = share_token(P.tokens, g.steps, &P.per_warp);
   int64_t blocks = ((int64_t)P.tokens + WARPS - 1) / WARPS * P.share;
   const int64_t most = (int64_t)GRAD_BLOCKS_PER_SM * mst_sm_count();
   if (blocks > most) blocks = most;
@@ -335,10 +336,10 @@ mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaSt
 template <typename T, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
   switch (lanes_of(P.R.D)) {
+    case 2: return launch_grad<T, 2, INTER>(P, dgamma_q, dgamma_k, s);
     case 4: return launch_grad<T, 4, INTER>(P, dgamma_q, dgamma_k, s);
     case 8: return launch_grad<T, 8, INTER>(P, dgamma_q, dgamma_k, s);
-    case 16: return launch_grad<T, 16, INTER>(P, dgamma_q, dgamma_k, s);
-    default: return launch_grad<T, 32, INTER>(P, dgamma_q, dgamma_k, s);
+    default: return launch_grad<T, 16, INTER>(P, dgamma_q, dgamma_k, s);
   }
 }
 template <typename T>

@@ -1,12 +1,13 @@
 // Norm and rotation of one head's row by a group of lanes: shared by the training calls and the append to a paged cache.
 //
-// A row of D = 8 .. 256 values lies in the registers of G neighbouring lanes, four pairs (u, v) a lane: two runs of four values, `near` and
+// A row of D = 8 .. 256 values lies in the registers of G neighbouring lanes, eight pairs (u, v) a lane: two runs of eight values, `near` and
 // `far` elements into the row.  Where pairs are halves apart the runs are rot / 2 apart, so both values of a pair are in one lane and nothing
 // is exchanged but the sum of squares (log2 G shuffles); neighbouring pairs lie within a run.  Values that do not turn fill further lanes
 // with runs of their own.  Two values that go through the same step share an instruction (f32x2).  With c, s the cosine and sine of the
 // pair's angle and r = 1 / sqrt(mean(x^2) + eps)
 //   u' = r (u gamma_u c - v gamma_v s),   v' = r (u gamma_u s + v gamma_v c)
-// where the products of weights and angles change with the token and the side (queries, keys) only, not from head to head.
+// A group of lanes keeps to one side, queries or keys, so the products of weights and angles are formed once a token.  (With eight values a lane
+// and groups that changed sides, a token of 24 rows took 1156 instructions, which was what 16384 of them waited for: 29 us.)
 #pragma once
 #include <cuda_bf16.h>
 
@@ -37,88 +38,104 @@ inline mst_status_t check(const mst_rotation_t* r, Rotation* out) {
   *out = Rotation{r->head_dim, r->rot_dim, r->interleaved != 0, r->eps, r->inv_freq, r->gamma_q, r->gamma_k};
   return MST_OK;
 }
-// lanes of a row: D / 8 of them have values; rows of up to 32 values share a kernel
-inline int lanes_of(int D) { return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32; }
+// lanes of a row: D / 16 of them have values; rows of up to 32 values share a kernel
+inline int lanes_of(int D) { return D <= 32 ? 2 : D <= 64 ? 4 : D <= 128 ? 8 : 16; }
 
 // ---------------------------------------------------------------------------------------------- a lane's part of a row
 struct Lane {
-  int near, far;    // first elements of its two runs
-  bool in, turns;
+  int near, far;    // first elements of its two runs of eight
+  bool in, in_far, turns;
   __device__ __forceinline__ Lane(const Rotation& R, int li, bool inter) {
-    in = 8 * li < R.D;
-    turns = 8 * li < R.rot;
-    if (inter) {
+    in = 16 * li < R.D;
+    turns = 16 * li < R.rot;
+    if (!inter && turns) {
       near = 8 * li;
-      far = near + 4;
-    } else if (turns) {
-      near = 4 * li;
       far = near + R.rot / 2;
     } else {
-      near = R.rot + 4 * (li - R.rot / 8);
-      far = near + (R.D - R.rot) / 2;
+      near = 16 * li;
+      far = near + 8;
     }
     if (!in) near = far = 0;
+    in_far = in && far < R.D;
+    if (!in_far) far = near;
   }
 };
 template <typename T>
 struct Raw {
-  uint32_t w[sizeof(T) * 2];
+  uint32_t w[sizeof(T) * 4];
 };
-__device__ __forceinline__ void load_row(Raw<__nv_bfloat16>& r, const __nv_bfloat16* p, const Lane& L) {
-  const uint2 a = *reinterpret_cast<const uint2*>(p + L.near), b = *reinterpret_cast<const uint2*>(p + L.far);
-  r.w[0] = a.x; r.w[1] = a.y; r.w[2] = b.x; r.w[3] = b.y;
+template <typename T>
+__device__ __forceinline__ void load_row(Raw<T>& r, const T* p, const Lane& L) {
+  constexpr int N = sizeof(T) * 2;      // words of a run
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p + L.near) + i);
+    r.w[i] = a.x; r.w[i + 1] = a.y; r.w[i + 2] = a.z; r.w[i + 3] = a.w;
+  }
+  if (L.in_far) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p + L.far) + i);
+      r.w[N + i] = a.x; r.w[N + i + 1] = a.y; r.w[N + i + 2] = a.z; r.w[N + i + 3] = a.w;
+    }
+  }
 }
-__device__ __forceinline__ void load_row(Raw<float>& r, const float* p, const Lane& L) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p + L.near), b = *reinterpret_cast<const uint4*>(p + L.far);
-  r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
-  r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
-}
-__device__ __forceinline__ void store_row(const Raw<__nv_bfloat16>& r, __nv_bfloat16* p, const Lane& L) {
-  *reinterpret_cast<uint2*>(p + L.near) = make_uint2(r.w[0], r.w[1]);
-  *reinterpret_cast<uint2*>(p + L.far) = make_uint2(r.w[2], r.w[3]);
-}
-__device__ __forceinline__ void store_row(const Raw<float>& r, float* p, const Lane& L) {
-  *reinterpret_cast<uint4*>(p + L.near) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
-  *reinterpret_cast<uint4*>(p + L.far) = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+template <typename T>
+__device__ __forceinline__ void store_row(const Raw<T>& r, T* p, const Lane& L) {
+  constexpr int N = sizeof(T) * 2;
+#pragma unroll
+  for (int i = 0; i < N; i += 4)
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p + L.near) + i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
+  if (L.in_far) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p + L.far) + i) = make_uint4(r.w[N + i], r.w[N + i + 1], r.w[N + i + 2], r.w[N + i + 3]);
+  }
 }
 template <typename T>
 __device__ __forceinline__ void no_row(Raw<T>& r) {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) * 2; ++i) r.w[i] = 0u;
+  for (int i = 0; i < (int)sizeof(T) * 4; ++i) r.w[i] = 0u;
 }
 
-// Four pairs, two to a register pair: u and v hold values 0, 1 and 2, 3
+// Eight pairs, two to a register pair
 struct Pairs {
-  uint64_t u[2], v[2];
+  uint64_t u[4], v[4];
 };
-// eight values in the order of memory (two runs of four) <-> pairs
+// sixteen values in the order of memory (two runs of eight) <-> pairs
 template <bool INTER>
-__device__ __forceinline__ Pairs pairs_of(const float (&x)[8]) {
+__device__ __forceinline__ Pairs pairs_of(const float (&x)[16]) {
   Pairs p;
-  if (INTER) {
-    p.u[0] = pack2(x[0], x[2]); p.v[0] = pack2(x[1], x[3]);
-    p.u[1] = pack2(x[4], x[6]); p.v[1] = pack2(x[5], x[7]);
-  } else {
-    p.u[0] = pack2(x[0], x[1]); p.u[1] = pack2(x[2], x[3]);
-    p.v[0] = pack2(x[4], x[5]); p.v[1] = pack2(x[6], x[7]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (INTER) {
+      p.u[k] = pack2(x[4 * k], x[4 * k + 2]);
+      p.v[k] = pack2(x[4 * k + 1], x[4 * k + 3]);
+    } else {
+      p.u[k] = pack2(x[2 * k], x[2 * k + 1]);
+      p.v[k] = pack2(x[8 + 2 * k], x[8 + 2 * k + 1]);
+    }
   }
   return p;
 }
 template <bool INTER>
-__device__ __forceinline__ void values_of(const Pairs& p, float (&x)[8]) {
-  if (INTER) {
-    unpack2(p.u[0], x[0], x[2]); unpack2(p.v[0], x[1], x[3]);
-    unpack2(p.u[1], x[4], x[6]); unpack2(p.v[1], x[5], x[7]);
-  } else {
-    unpack2(p.u[0], x[0], x[1]); unpack2(p.u[1], x[2], x[3]);
-    unpack2(p.v[0], x[4], x[5]); unpack2(p.v[1], x[6], x[7]);
+__device__ __forceinline__ void values_of(const Pairs& p, float (&x)[16]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (INTER) {
+      unpack2(p.u[k], x[4 * k], x[4 * k + 2]);
+      unpack2(p.v[k], x[4 * k + 1], x[4 * k + 3]);
+    } else {
+      unpack2(p.u[k], x[2 * k], x[2 * k + 1]);
+      unpack2(p.v[k], x[8 + 2 * k], x[8 + 2 * k + 1]);
+    }
   }
 }
 template <bool INTER>
 __device__ __forceinline__ Pairs widen(const Raw<__nv_bfloat16>& r) {
-  float x[8];
+  float x[16];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     x[2 * i] = __uint_as_float(r.w[i] << 16);
     x[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
   }
@@ -126,34 +143,38 @@ __device__ __forceinline__ Pairs widen(const Raw<__nv_bfloat16>& r) {
 }
 template <bool INTER>
 __device__ __forceinline__ Pairs widen(const Raw<float>& r) {
-  float x[8];
+  float x[16];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.w[i]);
+  for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r.w[i]);
   return pairs_of<INTER>(x);
 }
 template <bool INTER>
 __device__ __forceinline__ void narrow(const Pairs& p, Raw<__nv_bfloat16>& r) {
-  float x[8];
+  float x[16];
   values_of<INTER>(p, x);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  for (int i = 0; i < 8; ++i) r.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
 }
 template <bool INTER>
 __device__ __forceinline__ void narrow(const Pairs& p, Raw<float>& r) {
-  float x[8];
+  float x[16];
   values_of<INTER>(p, x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(x[i]);
+  for (int i = 0; i < 16; ++i) r.w[i] = __float_as_uint(x[i]);
 }
 // a lane's norm weights (ones where there is no norm or no value)
 template <bool INTER>
 __device__ __forceinline__ Pairs weights(const float* gamma, const Lane& L) {
-  float x[8];
+  float x[16];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 1.f;
+  for (int e = 0; e < 16; ++e) x[e] = 1.f;
   if (gamma && L.in) {
-    const float4 a = *reinterpret_cast<const float4*>(gamma + L.near), b = *reinterpret_cast<const float4*>(gamma + L.far);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      const float4 a = *reinterpret_cast<const float4*>(gamma + L.near + i), b = *reinterpret_cast<const float4*>(gamma + L.far + i);
+      x[i] = a.x; x[i + 1] = a.y; x[i + 2] = a.z; x[i + 3] = a.w;
+      x[8 + i] = b.x; x[8 + i + 1] = b.y; x[8 + i + 2] = b.z; x[8 + i + 3] = b.w;
+    }
   }
   return pairs_of<INTER>(x);
 }
@@ -163,7 +184,13 @@ __device__ __forceinline__ float halves_sum(uint64_t v) {
   return a + b;
 }
 __device__ __forceinline__ float dot(const Pairs& a, const Pairs& b) {
-  return halves_sum(add2(fma2(a.u[0], b.u[0], mul2(a.v[0], b.v[0])), fma2(a.u[1], b.u[1], mul2(a.v[1], b.v[1]))));
+  uint64_t s = mul2(a.u[0], b.u[0]), t = mul2(a.v[0], b.v[0]);
+#pragma unroll
+  for (int k = 1; k < 4; ++k) {
+    s = fma2(a.u[k], b.u[k], s);
+    t = fma2(a.v[k], b.v[k], t);
+  }
+  return halves_sum(add2(s, t));
 }
 template <int G>
 __device__ __forceinline__ float sum_lanes(float v) {
@@ -176,7 +203,7 @@ __device__ __forceinline__ float sum_lanes(float v) {
 // Cosines and sines of a position into a warp's own table, and out of it those of the lane's pairs.  The angle in turns, position * inv_freq /
 // 2 pi, is formed in fp64 and loses its whole part there: 53 bits hold 2^31 turns to 2^-22, and what is left goes to sincospi in fp32.
 struct Turn {
-  uint64_t c[2], s[2];
+  uint64_t c[4], s[4];
 };
 template <bool INTER>
 __device__ __forceinline__ Turn turn_of(float2* table, const Rotation& R, const Lane& L, int pos, int lane) {
@@ -189,24 +216,38 @@ __device__ __forceinline__ Turn turn_of(float2* table, const Rotation& R, const 
   }
   __syncwarp();
   Turn t;
-  t.c[0] = t.c[1] = pack2(1.f, 1.f);
-  t.s[0] = t.s[1] = 0ULL;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    t.c[k] = pack2(1.f, 1.f);
+    t.s[k] = 0ULL;
+  }
   if (L.turns) {
     const float4* at = reinterpret_cast<const float4*>(table + (INTER ? L.near / 2 : L.near));
-    const float4 a = at[0], b = at[1];
-    t.c[0] = pack2(a.x, a.z); t.s[0] = pack2(a.y, a.w);
-    t.c[1] = pack2(b.x, b.z); t.s[1] = pack2(b.y, b.w);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 a = at[k];
+      t.c[k] = pack2(a.x, a.z);
+      t.s[k] = pack2(a.y, a.w);
+    }
   }
   return t;
 }
 __device__ __forceinline__ uint64_t negated(uint64_t v) { return v ^ 0x8000000080000000ULL; }
 
-// A warp's steps through a token: 32 / G rows each, first the queries', then the keys', then the values' (which are only carried along).
-struct Steps {
-  int q, k, v;
-  __host__ __device__ Steps(int rows, int hq, int hk, int hv) : q((hq + rows - 1) / rows), k((hk + rows - 1) / rows), v((hv + rows - 1) / rows) {}
-  __host__ __device__ int all() const { return q + k + v; }
+// A warp's groups of lanes: the first `q` take the queries' rows in turn, the others the keys', as many of each as make the fewest steps.
+struct Groups {
+  int q, steps;
 };
+inline Groups groups_of(int lanes, int hq, int hk) {
+  const int all = 32 / lanes;
+  if (hq == 0 || hk == 0) return Groups{hq == 0 ? 0 : all, (hq + hk + all - 1) / all};
+  Groups best = {0, 1 << 30};
+  for (int q = 1; q < all; ++q) {
+    const int a = (hq + q - 1) / q, b = (hk + all - q - 1) / (all - q), steps = a > b ? a : b;
+    if (steps < best.steps) best = Groups{q, steps};
+  }
+  return best;
+}
 // Tokens alone fill the GPU from some thousands on; below that a token's steps are shared out, so that a few tokens are not a few warps' long
 // chains of loads.  Returns the warps of a token and sets their steps.
 inline int share_token(int64_t tokens, int steps, int* per_warp) {
