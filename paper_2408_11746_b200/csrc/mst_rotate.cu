@@ -28,7 +28,7 @@ struct RowsParams {
 
 template <typename T, int G, bool INTER, bool APPEND>
 __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid_constant__ RowsParams P) {
-  constexpr int AHEAD = sizeof(T) == 2 ? 3 : 2;      // steps whose loads are in flight together
+  constexpr int N = 4, AHEAD = sizeof(T) == 2 ? 3 : 2;      // steps whose loads are in flight together
   constexpr int ALL = 32 / G;
   __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
   const int token = (int)at;
   const int begin = (int)blockIdx.y * P.per_warp, all_end = begin + P.per_warp;
   const int end = all_end < P.steps ? all_end : P.steps;
-  const Lane L(P.R, lane % G, INTER);
+  const Lane L(P.R, lane % G, INTER, 2 * N);
   // this lane's side: its group's first head and how far apart its heads are
   const int group = lane / G;
   const bool is_q = group < P.groups_q;
@@ -47,14 +47,15 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
   const T* in = (const T*)(is_q ? P.Q : P.K) + token * P.ld + (int64_t)head0 * P.R.D;
   const int in_step = every * P.R.D;
   auto mine = [&](int i) { return i < end && L.in && head0 + i * every < heads; };
-  Raw<T> raw[AHEAD];
+  Raw<T, N> raw[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
     no_row(raw[u]);
     if (mine(begin + u)) load_row(raw[u], in + (int64_t)(begin + u) * in_step, L);
   }
   const float* gamma = is_q ? P.R.gamma_q : P.R.gamma_k;
-  const Pairs g = weights<INTER>(gamma, L);
+  const Pairs<N> g = weights<INTER, N>(gamma, L);
+  const Frequencies F(P.R, lane);
   int pos;
   mst_paged::Slot slot = {true, 0};
   if (APPEND) {
@@ -72,11 +73,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
                       : (T*)(is_q ? P.Qo : P.Ko) + token * P.ldq + (int64_t)head0 * P.R.D;
     const int64_t out_step = to_cache ? every * P.cache.head_stride : (int64_t)in_step;
     const bool writes = !to_cache || slot.exists;
-    Pairs A, B;      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
+    Pairs<N> A, B;      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
     {
-      const Turn turn = turn_of<INTER>(tables[warp], P.R, L, pos, lane);
+      const Turn<N> turn = turn_of<INTER, N>(tables[warp], P.R, F, L, pos, lane);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < N; ++k) {
         A.u[k] = mul2(g.u[k], turn.c[k]);
         A.v[k] = mul2(g.u[k], turn.s[k]);
         B.u[k] = negated(mul2(g.v[k], turn.s[k]));
@@ -90,17 +91,17 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
       for (int u = 0; u < AHEAD; ++u) {
         const int i = i0 + u;
         if (i >= end) break;
-        const Pairs x = widen<INTER>(raw[u]);
+        const Pairs<N> x = widen<INTER, N>(raw[u]);
         if (mine(i + AHEAD)) load_row(raw[u], in + (int64_t)(i + AHEAD) * in_step, L);
-        Pairs y;
+        Pairs<N> y;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N; ++k) {
           y.u[k] = mul2(x.u[k], A.u[k]);
           y.v[k] = mul2(x.v[k], B.v[k]);
         }
         if (!alone) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
+          for (int k = 0; k < N; ++k) {
             y.u[k] = fma2(x.v[k], B.u[k], y.u[k]);
             y.v[k] = fma2(x.u[k], A.v[k], y.v[k]);
           }
@@ -109,13 +110,13 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
         const float r = norm ? rsqrtf(fmaf(sum, inv_d, P.R.eps)) : 1.f;
         const uint64_t r2 = pack2(r, r);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N; ++k) {
           y.u[k] = mul2(y.u[k], r2);
           y.v[k] = mul2(y.v[k], r2);
         }
         if (mine(i) && writes) {
-          Raw<T> o;
-          narrow<INTER>(y, o);
+          Raw<T, N> o;
+          narrow<INTER, N>(y, o);
           store_row(o, out + i * out_step, L);
         }
       }
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
     for (int i = v0; i < v1; ++i) {
       const int head = i * ALL + group;
       if (head < P.hk && L.in) {
-        Raw<T> r;
+        Raw<T, N> r;
         load_row(r, from + (int64_t)head * P.R.D, L);
         store_row(r, to + head * P.cache.head_stride, L);
       }
@@ -155,15 +156,15 @@ struct GradParams {
 constexpr int GRAD_BLOCKS_PER_SM = 2;
 constexpr int GRAD_BLOCKS_MOST = 512;
 
-template <typename T, int G, bool INTER>
+template <typename T, int G, int N, bool INTER>
 __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_kernel(const __grid_constant__ GradParams P) {
-  constexpr int ALL = 32 / G;
+  constexpr int ALL = 32 / G, AHEAD = sizeof(T) * N <= 4 ? 3 : 1;
   __shared__ __align__(16) float2 tables[WARPS][MAX_HALF];
   __shared__ float sums[WARPS][2][256];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
-  const Lane L(P.R, lane % G, INTER);
+  const Lane L(P.R, lane % G, INTER, 2 * N);
   const int group = lane / G;
   const bool is_q = group < P.groups_q;
   const int head0 = is_q ? group : group - P.groups_q, every = is_q ? P.groups_q : ALL - P.groups_q, heads = is_q ? P.hq : P.hk;
@@ -171,8 +172,9 @@ __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_ke
   const float* gamma = is_q ? P.R.gamma_q : P.R.gamma_k;
   const bool norm = gamma != nullptr, alone = !L.turns;
   const float inv_d = 1.f / (float)P.R.D;
-  const Pairs g = weights<INTER>(gamma, L);
-  Pairs acc = {};
+  const Pairs<N> g = weights<INTER, N>(gamma, L);
+  const Frequencies F(P.R, lane);
+  Pairs<N> acc = {};
   const unsigned groups = ((unsigned)P.tokens + WARPS - 1) / WARPS, all = groups * (unsigned)P.share;
   for (unsigned unit = blockIdx.x; unit < all; unit += gridDim.x) {
     const unsigned part = P.share > 1 ? unit / groups : 0u, at = (unit - part * groups) * WARPS + warp;
@@ -185,58 +187,66 @@ __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_ke
     const T* y_in = (const T*)(is_q ? P.dQo : P.dKo) + token * P.lddo + off;
     T* out = (T*)(is_q ? P.dQ : P.dK) + token * P.ldg + off;
     auto mine = [&](int i) { return i < end && L.in && head0 + i * every < heads; };
-    Raw<T> rx, ry;
-    auto fetch = [&](int i) {
+    Raw<T, N> rx[AHEAD], ry[AHEAD];
+    auto fetch = [&](int i, Raw<T, N>& x, Raw<T, N>& y) {
       if (mine(i)) {
-        load_row(ry, y_in + (int64_t)i * step, L);
-        if (norm) load_row(rx, x_in + (int64_t)i * step, L);
+        load_row(y, y_in + (int64_t)i * step, L);
+        if (norm) load_row(x, x_in + (int64_t)i * step, L);
       }
     };
-    no_row(rx);
-    no_row(ry);
-    fetch(begin);
-    const Turn turn = turn_of<INTER>(tables[warp], P.R, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
-    for (int i = begin; i < end; ++i) {
-      const bool here = mine(i);
-      const Pairs y = widen<INTER>(ry), x = widen<INTER>(rx);
-      fetch(i + 1);
-      Pairs z;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        z.u[k] = mul2(y.u[k], turn.c[k]);
-        z.v[k] = mul2(y.v[k], turn.c[k]);
-      }
-      if (!alone) {
+    for (int u = 0; u < AHEAD; ++u) {
+      no_row(rx[u]);
+      no_row(ry[u]);
+      fetch(begin + u, rx[u], ry[u]);
+    }
+    const Turn<N> turn = turn_of<INTER, N>(tables[warp], P.R, F, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
+    for (int i0 = begin; i0 < end; i0 += AHEAD) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          z.u[k] = fma2(y.v[k], turn.s[k], z.u[k]);
-          z.v[k] = fma2(y.u[k], negated(turn.s[k]), z.v[k]);
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u;
+        if (i >= end) break;
+        const bool here = mine(i);
+        const Pairs<N> y = widen<INTER, N>(ry[u]), x = widen<INTER, N>(rx[u]);
+        fetch(i + AHEAD, rx[u], ry[u]);
+        Pairs<N> z;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          z.u[k] = mul2(y.u[k], turn.c[k]);
+          z.v[k] = mul2(y.v[k], turn.c[k]);
         }
-      }
-      Pairs zg;
+        if (!alone) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        zg.u[k] = mul2(z.u[k], g.u[k]);
-        zg.v[k] = mul2(z.v[k], g.v[k]);
-      }
-      const float sq = sum_lanes<G>(dot(x, x)), sd = sum_lanes<G>(dot(zg, x));     // every lane: they have shuffles
-      if (norm) {
-        const float r = rsqrtf(fmaf(sq, inv_d, P.R.eps)), back = -r * r * (sd * inv_d);
-        const uint64_t r2 = pack2(r, r), b2 = pack2(back, back);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (here) {       // rows that are not there may be another step's
-            acc.u[k] = fma2(z.u[k], mul2(x.u[k], r2), acc.u[k]);
-            acc.v[k] = fma2(z.v[k], mul2(x.v[k], r2), acc.v[k]);
+          for (int k = 0; k < N; ++k) {
+            z.u[k] = fma2(y.v[k], turn.s[k], z.u[k]);
+            z.v[k] = fma2(y.u[k], negated(turn.s[k]), z.v[k]);
           }
-          z.u[k] = mul2(r2, fma2(b2, x.u[k], zg.u[k]));
-          z.v[k] = mul2(r2, fma2(b2, x.v[k], zg.v[k]));
         }
-      }
-      if (here) {
-        Raw<T> o;
-        narrow<INTER>(z, o);
-        store_row(o, out + (int64_t)i * step, L);
+        Pairs<N> zg;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          zg.u[k] = mul2(z.u[k], g.u[k]);
+          zg.v[k] = mul2(z.v[k], g.v[k]);
+        }
+        const float sq = sum_lanes<G>(dot(x, x)), sd = sum_lanes<G>(dot(zg, x));     // every lane: they have shuffles
+        if (norm) {
+          const float r = rsqrtf(fmaf(sq, inv_d, P.R.eps)), back = -r * r * (sd * inv_d);
+          const uint64_t r2 = pack2(r, r), b2 = pack2(back, back);
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            if (here) {       // rows that are not there may be another step's
+              acc.u[k] = fma2(z.u[k], mul2(x.u[k], r2), acc.u[k]);
+              acc.v[k] = fma2(z.v[k], mul2(x.v[k], r2), acc.v[k]);
+            }
+            z.u[k] = mul2(r2, fma2(b2, x.u[k], zg.u[k]));
+            z.v[k] = mul2(r2, fma2(b2, x.v[k], zg.v[k]));
+          }
+        }
+        if (here) {
+          Raw<T, N> o;
+          narrow<INTER, N>(z, o);
+          store_row(o, out + (int64_t)i * step, L);
+        }
       }
     }
   }
@@ -244,16 +254,16 @@ __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_ke
   // the groups of a warp, then the warps, in a fixed order
   for (int e = threadIdx.x; e < WARPS * 2 * 256; e += 32 * WARPS) (&sums[0][0][0])[e] = 0.f;
   __syncthreads();
-  float v[16];
-  values_of<INTER>(acc, v);
+  float v[4 * N];
+  values_of<INTER, N>(acc, v);
   float* to = sums[warp][is_q ? 0 : 1];
 #pragma unroll 1
   for (int k = 0; k < ALL; ++k) {
     if (group == k && L.in) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 2 * N; ++e) {
         to[L.near + e] += v[e];
-        if (L.in_far) to[L.far + e] += v[8 + e];
+        if (L.in_far) to[L.far + e] += v[2 * N + e];
       }
     }
     __syncwarp();
@@ -306,7 +316,7 @@ mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
 }
 template <typename T, bool INTER, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
-  switch (lanes_of(P.R.D)) {
+  switch (lanes_of(P.R.D, 4)) {
     case 2: return launch_rows<T, 2, INTER, APPEND>(P, s);
     case 4: return launch_rows<T, 4, INTER, APPEND>(P, s);
     case 8: return launch_rows<T, 8, INTER, APPEND>(P, s);
@@ -317,7 +327,7 @@ template <typename T, bool APPEND>
 mst_status_t launch_rows(RowsParams& P, cudaStream_t s) {
   return P.R.inter ? launch_rows<T, true, APPEND>(P, s) : launch_rows<T, false, APPEND>(P, s);
 }
-template <typename T, int G, bool INTER>
+template <typename T, int G, int N, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
   const Groups g = groups_of(G, P.hq, P.hk);
   P.groups_q = g.q;
@@ -327,7 +337,7 @@ mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaSt
   const int64_t most = (int64_t)GRAD_BLOCKS_PER_SM * mst_sm_count();
   if (blocks > most) blocks = most;
   if (blocks > GRAD_BLOCKS_MOST) blocks = GRAD_BLOCKS_MOST;
-  MST_CUDA_TRY(mst_launch_overlapped(rotate_grad_kernel<T, G, INTER>, dim3((unsigned)blocks), dim3(32 * WARPS), 0, s, P));
+  MST_CUDA_TRY(mst_launch_overlapped(rotate_grad_kernel<T, G, N, INTER>, dim3((unsigned)blocks), dim3(32 * WARPS), 0, s, P));
   if (P.partial)
     MST_CUDA_TRY(mst_launch_overlapped(rotate_weight_grad_kernel, dim3((unsigned)((2 * P.R.D + 31) / 32)), dim3(1024), 0, s,
                                        (const float*)P.partial, (int)blocks, P.R.D, dgamma_q, dgamma_k));
@@ -335,11 +345,11 @@ mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaSt
 }
 template <typename T, bool INTER>
 mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaStream_t s) {
-  switch (lanes_of(P.R.D)) {
-    case 2: return launch_grad<T, 2, INTER>(P, dgamma_q, dgamma_k, s);
-    case 4: return launch_grad<T, 4, INTER>(P, dgamma_q, dgamma_k, s);
-    case 8: return launch_grad<T, 8, INTER>(P, dgamma_q, dgamma_k, s);
-    default: return launch_grad<T, 16, INTER>(P, dgamma_q, dgamma_k, s);
+  switch (lanes_of(P.R.D, 2)) {
+    case 4: return launch_grad<T, 4, 2, INTER>(P, dgamma_q, dgamma_k, s);
+    case 8: return launch_grad<T, 8, 2, INTER>(P, dgamma_q, dgamma_k, s);
+    case 16: return launch_grad<T, 16, 2, INTER>(P, dgamma_q, dgamma_k, s);
+    default: return launch_grad<T, 16, 4, INTER>(P, dgamma_q, dgamma_k, s);      // two groups in a warp at least: one for each side
   }
 }
 template <typename T>

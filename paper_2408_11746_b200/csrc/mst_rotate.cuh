@@ -1,7 +1,7 @@
 // Norm and rotation of one head's row by a group of lanes: shared by the training calls and the append to a paged cache.
 //
-// A row of D = 8 .. 256 values lies in the registers of G neighbouring lanes, eight pairs (u, v) a lane: two runs of eight values, `near` and
-// `far` elements into the row.  Where pairs are halves apart the runs are rot / 2 apart, so both values of a pair are in one lane and nothing
+// A row of D = 8 .. 256 values lies in the registers of G neighbouring lanes, 2 N pairs (u, v) a lane (N = 4 forward, 2 in the gradients, which hold
+// twice as much): two runs of 2 N values, `near` and `far` elements into the row.  Where pairs are halves apart the runs are rot / 2 apart, so both values of a pair are in one lane and nothing
 // is exchanged but the sum of squares (log2 G shuffles); neighbouring pairs lie within a run.  Values that do not turn fill further lanes
 // with runs of their own.  Two values that go through the same step share an instruction (f32x2).  With c, s the cosine and sine of the
 // pair's angle and r = 1 / sqrt(mean(x^2) + eps)
@@ -38,155 +38,164 @@ inline mst_status_t check(const mst_rotation_t* r, Rotation* out) {
   *out = Rotation{r->head_dim, r->rot_dim, r->interleaved != 0, r->eps, r->inv_freq, r->gamma_q, r->gamma_k};
   return MST_OK;
 }
-// lanes of a row: D / 16 of them have values; rows of up to 32 values share a kernel
-inline int lanes_of(int D) { return D <= 32 ? 2 : D <= 64 ? 4 : D <= 128 ? 8 : 16; }
+// lanes of a row: D / (4 N) of them have values; rows of up to 32 values share a kernel
+inline int lanes_of(int D, int N) { return (D <= 32 ? 8 : D <= 64 ? 16 : D <= 128 ? 32 : 64) / N; }
 
 // ---------------------------------------------------------------------------------------------- a lane's part of a row
 struct Lane {
-  int near, far;    // first elements of its two runs of eight
+  int near, far;    // first elements of its two runs of `run`
   bool in, in_far, turns;
-  __device__ __forceinline__ Lane(const Rotation& R, int li, bool inter) {
-    in = 16 * li < R.D;
-    turns = 16 * li < R.rot;
+  __device__ __forceinline__ Lane(const Rotation& R, int li, bool inter, int run) {
+    in = 2 * run * li < R.D;
+    turns = 2 * run * li < R.rot;
     if (!inter && turns) {
-      near = 8 * li;
+      near = run * li;
       far = near + R.rot / 2;
     } else {
-      near = 16 * li;
-      far = near + 8;
+      near = 2 * run * li;
+      far = near + run;
     }
     if (!in) near = far = 0;
     in_far = in && far < R.D;
     if (!in_far) far = near;
   }
 };
-template <typename T>
+template <typename T, int N>
 struct Raw {
-  uint32_t w[sizeof(T) * 4];
+  uint32_t w[sizeof(T) * N];
 };
-template <typename T>
-__device__ __forceinline__ void load_row(Raw<T>& r, const T* p, const Lane& L) {
-  constexpr int N = sizeof(T) * 2;      // words of a run
+// a run of 2 N values: 8 bytes or 16 at a time
+template <int WORDS>
+__device__ __forceinline__ void load_run(uint32_t* w, const void* p) {
+  if (WORDS == 2) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p);
+    w[0] = a.x; w[1] = a.y;
+  } else {
 #pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p + L.near) + i);
-    r.w[i] = a.x; r.w[i + 1] = a.y; r.w[i + 2] = a.z; r.w[i + 3] = a.w;
-  }
-  if (L.in_far) {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p + L.far) + i);
-      r.w[N + i] = a.x; r.w[N + i + 1] = a.y; r.w[N + i + 2] = a.z; r.w[N + i + 3] = a.w;
+    for (int i = 0; i + 4 <= WORDS; i += 4) {
+      const uint4 a = reinterpret_cast<const uint4*>(p)[i / 4];
+      w[i] = a.x; w[i + 1] = a.y; w[i + 2] = a.z; w[i + 3] = a.w;
     }
   }
 }
-template <typename T>
-__device__ __forceinline__ void store_row(const Raw<T>& r, T* p, const Lane& L) {
-  constexpr int N = sizeof(T) * 2;
+template <int WORDS>
+__device__ __forceinline__ void store_run(const uint32_t* w, void* p) {
+  if (WORDS == 2) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  } else {
 #pragma unroll
-  for (int i = 0; i < N; i += 4)
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p + L.near) + i) = make_uint4(r.w[i], r.w[i + 1], r.w[i + 2], r.w[i + 3]);
-  if (L.in_far) {
-#pragma unroll
-    for (int i = 0; i < N; i += 4)
-      *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(p + L.far) + i) = make_uint4(r.w[N + i], r.w[N + i + 1], r.w[N + i + 2], r.w[N + i + 3]);
+    for (int i = 0; i + 4 <= WORDS; i += 4) reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
   }
 }
-template <typename T>
-__device__ __forceinline__ void no_row(Raw<T>& r) {
+template <typename T, int N>
+__device__ __forceinline__ void load_row(Raw<T, N>& r, const T* p, const Lane& L) {
+  constexpr int W = sizeof(T) * N / 2;
+  load_run<W>(r.w, p + L.near);
+  if (L.in_far) load_run<W>(r.w + W, p + L.far);
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_row(const Raw<T, N>& r, T* p, const Lane& L) {
+  constexpr int W = sizeof(T) * N / 2;
+  store_run<W>(r.w, p + L.near);
+  if (L.in_far) store_run<W>(r.w + W, p + L.far);
+}
+template <typename T, int N>
+__device__ __forceinline__ void no_row(Raw<T, N>& r) {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T) * 4; ++i) r.w[i] = 0u;
+  for (int i = 0; i < (int)sizeof(T) * N; ++i) r.w[i] = 0u;
 }
 
-// Eight pairs, two to a register pair
+// 2 N pairs, two to a register pair
+template <int N>
 struct Pairs {
-  uint64_t u[4], v[4];
+  uint64_t u[N], v[N];
 };
-// sixteen values in the order of memory (two runs of eight) <-> pairs
-template <bool INTER>
-__device__ __forceinline__ Pairs pairs_of(const float (&x)[16]) {
-  Pairs p;
+// 4 N values in the order of memory (two runs) <-> pairs
+template <bool INTER, int N>
+__device__ __forceinline__ Pairs<N> pairs_of(const float (&x)[4 * N]) {
+  Pairs<N> p;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < N; ++k) {
     if (INTER) {
       p.u[k] = pack2(x[4 * k], x[4 * k + 2]);
       p.v[k] = pack2(x[4 * k + 1], x[4 * k + 3]);
     } else {
       p.u[k] = pack2(x[2 * k], x[2 * k + 1]);
-      p.v[k] = pack2(x[8 + 2 * k], x[8 + 2 * k + 1]);
+      p.v[k] = pack2(x[2 * N + 2 * k], x[2 * N + 2 * k + 1]);
     }
   }
   return p;
 }
-template <bool INTER>
-__device__ __forceinline__ void values_of(const Pairs& p, float (&x)[16]) {
+template <bool INTER, int N>
+__device__ __forceinline__ void values_of(const Pairs<N>& p, float (&x)[4 * N]) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < N; ++k) {
     if (INTER) {
       unpack2(p.u[k], x[4 * k], x[4 * k + 2]);
       unpack2(p.v[k], x[4 * k + 1], x[4 * k + 3]);
     } else {
       unpack2(p.u[k], x[2 * k], x[2 * k + 1]);
-      unpack2(p.v[k], x[8 + 2 * k], x[8 + 2 * k + 1]);
+      unpack2(p.v[k], x[2 * N + 2 * k], x[2 * N + 2 * k + 1]);
     }
   }
 }
-template <bool INTER>
-__device__ __forceinline__ Pairs widen(const Raw<__nv_bfloat16>& r) {
-  float x[16];
+template <bool INTER, int N>
+__device__ __forceinline__ Pairs<N> widen(const Raw<__nv_bfloat16, N>& r) {
+  float x[4 * N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 2 * N; ++i) {
     x[2 * i] = __uint_as_float(r.w[i] << 16);
     x[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
   }
-  return pairs_of<INTER>(x);
+  return pairs_of<INTER, N>(x);
 }
-template <bool INTER>
-__device__ __forceinline__ Pairs widen(const Raw<float>& r) {
-  float x[16];
+template <bool INTER, int N>
+__device__ __forceinline__ Pairs<N> widen(const Raw<float, N>& r) {
+  float x[4 * N];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r.w[i]);
-  return pairs_of<INTER>(x);
+  for (int i = 0; i < 4 * N; ++i) x[i] = __uint_as_float(r.w[i]);
+  return pairs_of<INTER, N>(x);
 }
-template <bool INTER>
-__device__ __forceinline__ void narrow(const Pairs& p, Raw<__nv_bfloat16>& r) {
-  float x[16];
-  values_of<INTER>(p, x);
+template <bool INTER, int N>
+__device__ __forceinline__ void narrow(const Pairs<N>& p, Raw<__nv_bfloat16, N>& r) {
+  float x[4 * N];
+  values_of<INTER, N>(p, x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+  for (int i = 0; i < 2 * N; ++i) r.w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
 }
-template <bool INTER>
-__device__ __forceinline__ void narrow(const Pairs& p, Raw<float>& r) {
-  float x[16];
-  values_of<INTER>(p, x);
+template <bool INTER, int N>
+__device__ __forceinline__ void narrow(const Pairs<N>& p, Raw<float, N>& r) {
+  float x[4 * N];
+  values_of<INTER, N>(p, x);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) r.w[i] = __float_as_uint(x[i]);
+  for (int i = 0; i < 4 * N; ++i) r.w[i] = __float_as_uint(x[i]);
 }
 // a lane's norm weights (ones where there is no norm or no value)
-template <bool INTER>
-__device__ __forceinline__ Pairs weights(const float* gamma, const Lane& L) {
-  float x[16];
+template <bool INTER, int N>
+__device__ __forceinline__ Pairs<N> weights(const float* gamma, const Lane& L) {
+  float x[4 * N];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) x[e] = 1.f;
+  for (int e = 0; e < 4 * N; ++e) x[e] = 1.f;
   if (gamma && L.in) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 4) {
+    for (int i = 0; i < 2 * N; i += 4) {
       const float4 a = *reinterpret_cast<const float4*>(gamma + L.near + i), b = *reinterpret_cast<const float4*>(gamma + L.far + i);
       x[i] = a.x; x[i + 1] = a.y; x[i + 2] = a.z; x[i + 3] = a.w;
-      x[8 + i] = b.x; x[8 + i + 1] = b.y; x[8 + i + 2] = b.z; x[8 + i + 3] = b.w;
+      x[2 * N + i] = b.x; x[2 * N + i + 1] = b.y; x[2 * N + i + 2] = b.z; x[2 * N + i + 3] = b.w;
     }
   }
-  return pairs_of<INTER>(x);
+  return pairs_of<INTER, N>(x);
 }
 __device__ __forceinline__ float halves_sum(uint64_t v) {
   float a, b;
   unpack2(v, a, b);
   return a + b;
 }
-__device__ __forceinline__ float dot(const Pairs& a, const Pairs& b) {
+template <int N>
+__device__ __forceinline__ float dot(const Pairs<N>& a, const Pairs<N>& b) {
   uint64_t s = mul2(a.u[0], b.u[0]), t = mul2(a.v[0], b.v[0]);
 #pragma unroll
-  for (int k = 1; k < 4; ++k) {
+  for (int k = 1; k < N; ++k) {
     s = fma2(a.u[k], b.u[k], s);
     t = fma2(a.v[k], b.v[k], t);
   }
@@ -202,29 +211,40 @@ __device__ __forceinline__ float sum_lanes(float v) {
 // ---------------------------------------------------------------------------------------------- the turn
 // Cosines and sines of a position into a warp's own table, and out of it those of the lane's pairs.  The angle in turns, position * inv_freq /
 // 2 pi, is formed in fp64 and loses its whole part there: 53 bits hold 2^31 turns to 2^-22, and what is left goes to sincospi in fp32.
-struct Turn {
-  uint64_t c[4], s[4];
+// A lane keeps the frequencies that it sees to: lane, lane + 32, .. of rot / 2.
+struct Frequencies {
+  float f[MAX_HALF / 32];
+  __device__ __forceinline__ Frequencies(const Rotation& R, int lane) {
+#pragma unroll
+    for (int k = 0; k < MAX_HALF / 32; ++k) f[k] = lane + 32 * k < R.rot / 2 ? R.inv_freq[lane + 32 * k] : 0.f;
+  }
 };
-template <bool INTER>
-__device__ __forceinline__ Turn turn_of(float2* table, const Rotation& R, const Lane& L, int pos, int lane) {
+template <int N>
+struct Turn {
+  uint64_t c[N], s[N];
+};
+template <bool INTER, int N>
+__device__ __forceinline__ Turn<N> turn_of(float2* table, const Rotation& R, const Frequencies& F, const Lane& L, int pos, int lane) {
   __syncwarp();
-  for (int i = lane; i < R.rot / 2; i += 32) {
-    const double turns = (double)pos * ((double)R.inv_freq[i] * 0.15915494309189533577);
+#pragma unroll
+  for (int k = 0; k < MAX_HALF / 32; ++k) {
+    if (32 * k >= R.rot / 2) break;
+    const double turns = (double)pos * ((double)F.f[k] * 0.15915494309189533577);
     float2 v;
     sincospif((float)(2.0 * (turns - rint(turns))), &v.y, &v.x);
-    table[i] = v;
+    table[lane + 32 * k] = v;
   }
   __syncwarp();
-  Turn t;
+  Turn<N> t;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < N; ++k) {
     t.c[k] = pack2(1.f, 1.f);
     t.s[k] = 0ULL;
   }
   if (L.turns) {
     const float4* at = reinterpret_cast<const float4*>(table + (INTER ? L.near / 2 : L.near));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N; ++k) {
       const float4 a = at[k];
       t.c[k] = pack2(a.x, a.z);
       t.s[k] = pack2(a.y, a.w);
