@@ -393,19 +393,23 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   const int64_t tiles = (rows + p.rows - 1) / p.rows, most = 65535;
   p.count = (int)(tiles < most ? tiles : most);
-  // units of the longest list: 64 entries, or tiles of 128 keys
+  // units of the longest list: 64 entries; or tiles of 128 keys and strided keys, which take about as long
   const int64_t in_tile = (p.rows + group - 1) / group, nt = b.max_new < in_tile ? (b.max_new > 0 ? b.max_new : 1) : in_tile;
   int64_t units;
+  int waves;      // of blocks, two of which an SM holds, that ranges are cut for
+  p.least = 8;
   if (p.tiles) {
-    units = (stride >= len || stride < DENSE_BELOW ? len : stride + nt < len ? stride + nt : len) / KEYS_OF_TILE + 1;
-    p.least = 8;
+    const bool dense = stride < DENSE_BELOW;
+    const int64_t near = (dense || stride + nt > len ? len : stride + nt) / KEYS_OF_TILE + 1, far = dense ? 0 : len / stride;
+    units = near + far;
+    waves = 1;
   } else {
     const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
     units = (list + UNIT - 1) / UNIT;
-    p.least = 8;
+    waves = 2;
   }
-  const int64_t blocks = lists * tiles, want = (p.tiles ? 8 : 4) * (int64_t)mst_sm_count();
-  int64_t splits = (want + blocks - 1) / blocks;
+  const int64_t blocks = lists * tiles, want = 2 * waves * (int64_t)mst_sm_count();
+  int64_t splits = p.tiles ? want / blocks : (want + blocks - 1) / blocks;
   const int64_t fit = (units + p.least - 1) / p.least;
   if (splits > fit) splits = fit;
   if (splits > 64) splits = 64;

@@ -129,14 +129,16 @@ struct TileWalk {
     near = T.p_hi < 0 ? 0 : last >= first ? (int)((last - first) / KEYS_OF_TILE) + 1 : 1;
     far = dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - 1;
   }
-  // Range `split`: near tiles n0 .. n1 - 1, strided keys m0 .. m1 - 1 steps behind.  active: how many ranges there are, each with a near tile.
+  // Range `split` of at most `splits` equal ranges, each with `least` tiles and steps or more and a near tile: near tiles n0 .. n1 - 1, strided keys
+  // m0 .. m1 - 1 steps behind.  active: how many ranges there are.
   MST_HD bool range(int splits, int least, int split, int& n0, int& n1, int& m0, int& m1, int& active) const {
-    int each = near / splits + (near % splits != 0);
-    if (each < least) each = least;
-    active = near == 0 ? 1 : near / each + (near % each != 0);
+    const int64_t parts = ((int64_t)near + far + least - 1) / least;
+    active = (int)(parts < splits ? parts : splits);
+    if (active > near) active = near;
+    if (active < 1) active = 1;
     if (split >= active) return false;
-    n0 = split * each;
-    n1 = near - n0 < each ? near : n0 + each;
+    n0 = (int)((int64_t)near * split / active);
+    n1 = (int)((int64_t)near * (split + 1) / active);
     m0 = 2 + (int)((int64_t)far * split / active);
     m1 = 2 + (int)((int64_t)far * (split + 1) / active);
     return true;

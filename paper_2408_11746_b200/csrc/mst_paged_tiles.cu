@@ -46,25 +46,8 @@ struct TileParams {
   int at_slot, at_head, at_page;   // which of the map's coordinates 1 .. 3 they are
 };
 
-// mbar_wait, but asleep in the barrier for up to 2 us at a time: the warps that wait here share their schedulers with those that count
 __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  for (uint32_t it = 0;; ++it) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(2000u)
-        : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
-    if (it > MST_SPIN_LIMIT / 4) {
-      *abort_flag = 1;
-      atomicOr(&g_wait_error, 1);
-      return false;
-    }
-  }
+  return mbar_wait(bar, parity, abort_flag, &g_wait_error);
 }
 constexpr float MOST = 65536.f;
 __device__ __forceinline__ float halves_sum(uint64_t v) {
@@ -86,6 +69,18 @@ __device__ __forceinline__ uint32_t elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(one));
   return one;
+}
+__device__ __forceinline__ void tmem_ld8_nowait(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld8_wait(uint32_t (&r)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+               :
+               : "memory");
 }
 // The instructions of a whole warp of which the elected lane's counts: no branch around them, so that what they name stays uniform
 __device__ __forceinline__ void mma_ss(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t accum) {
@@ -229,18 +224,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         }
       continue;
     }
-    // do all the range's pages exist (keys behind a sequence's end are behind every row of it)
     const int32_t* table = P.B.table + (int64_t)b * P.B.table_stride;
-    bool hole = len > reach;
-    {
-      const int64_t end = (int64_t)key0 + (int64_t)near * KEYS;
-      const int p1 = have > 0 ? ((int)(end < have ? end : have) - 1) / P.C.page_size : -1;
-      for (int p = key0 / P.C.page_size + (int)threadIdx.x; p <= p1; p += THREADS) {
-        const int id = table[p];
-        hole = hole || id < 0 || id >= P.C.num_pages;
-      }
-    }
-    hole = __syncthreads_or(hole) != 0;
     // A wait that gives up sets the block's abort flag, after which every wait returns at once: nobody leaves his loop early, and nothing is stored
     if (warp == CW) {
       // ------------------------------------------------------------------------------------------ loads
@@ -288,7 +272,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               tma_load_4d(to_k + (uint32_t)(q * 2 * TILE_BYTES + lane * A.box * 128), &tmK, 64 * q, c[1], c[2], c[3], full_k + 8 * s);
           if (n >= STAGES) wait_on(empty_v + 8 * s, before, abort_flag);     // then nobody reads `exist` of the tile before either
           __syncwarp();
-          if (lane < 4 && hole) exist[4 * s + lane] = ~0u;
+          if (lane < 4) exist[4 * s + lane] = ~0u;
           __syncwarp();
           if (lane == 0) mbar_expect_tx(full_v + 8 * s, S::SLOT_BYTES);
           __syncwarp();
@@ -370,24 +354,17 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       };
       constexpr std::integral_constant<uint32_t, 0> C0{};
       constexpr std::integral_constant<uint32_t, 1> C1{};
-      auto keys_in = [&](uint32_t n) {
-        wait_on(full_k + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
-        __syncwarp();
-        tc_fence_after();
-      };
       // tile j in slot `here`: its weights are used up half by half, the next tile's scores follow in the other slot
       auto turn = [&](int j, auto here, auto there) {
         const uint32_t n = base_t + (uint32_t)j;
         const bool last = j + 1 == near;
-        wait_on(full_v + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);
+        wait_on(full_v + 8 * (n % STAGES), (n / STAGES) & 1u, abort_flag);     // ahead of the weights: nothing but products between those and the scores
+        if (!last) wait_on(full_k + 8 * ((n + 1) % STAGES), ((n + 1) / STAGES) & 1u, abort_flag);
         wait_on(p_full, n & 1u, abort_flag);
         __syncwarp();
         tc_fence_after();
         outputs(here, C0, (j > 0 ? 1u : 0u) | from_far, last);
-        if (!last) {
-          keys_in(n + 1);
-          scores(there, C0);
-        }
+        if (!last) scores(there, C0);
         wait_on(p_full + 8, n & 1u, abort_flag);
         __syncwarp();
         tc_fence_after();
@@ -396,7 +373,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       };
       static_assert(STAGES == 2, "slots take turns");
       wait_on(own_full, lap & 1u, abort_flag);
-      keys_in(base_t);
+      wait_on(full_k + 8 * (base_t % STAGES), (base_t / STAGES) & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
       if (base_t % 2 == 0) {
         scores(C0, C0);
         scores(C0, C1);
@@ -419,6 +398,23 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const int pos = live ? T.p_lo + (T.row0 + r) / P.group - T.t_lo : -1;
       const int w0 = quarter * 32, w1 = w0 + 31 < T.rows ? w0 + 31 : T.rows - 1;     // this warp's rows
       const int i_lo = T.p_lo + (T.row0 + w0) / P.group - T.t_lo, i_hi = w0 < T.rows ? T.p_lo + (T.row0 + w1) / P.group - T.t_lo : -1;
+      // do all the range's pages exist (keys behind a sequence's end are behind every row of it)
+      bool hole = len > reach;
+      {
+        const int64_t stop = (int64_t)key0 + (int64_t)near * KEYS;
+        const int p1 = have > 0 ? P.C.by_page.over((int)(stop < have ? stop : have) - 1) : -1;
+        for (int p = P.C.by_page.over(key0) + (int)threadIdx.x; p <= p1; p += 32 * CW) {
+          const int id = table[p];
+          hole = hole || id < 0 || id >= P.C.num_pages;
+        }
+        uint32_t any_hole;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 2, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+            : "=r"(any_hole)
+            : "r"((uint32_t)hole)
+            : "memory");
+        hole = any_hole != 0u;
+      }
       float m = -INFINITY;                                   // reference of this half's softmax, base 2
       float total_w = 0.f;
       if (MODE == FAR && m1 > m0) {
@@ -431,16 +427,30 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         float acc[HALF], fm = -INFINITY, fs = 0.f;
 #pragma unroll
         for (int e = 0; e < HALF; ++e) acc[e] = 0.f;
-        for (int k = m0; k < m1; ++k) {
+        // A step's page is asked for a step ahead, its slot's place in the cache is worked out when the number is there
+        struct Far { int id, slot; };
+        auto look = [&](int k) {
           const int64_t j = (int64_t)fp - (int64_t)k * P.l;
-          Slot sl = {false, 0};
-          if (j >= 0) sl = slot_of(P.C, P.B, b, (int)j, &g_bad_page);
-          const int64_t at = sl.at + (int64_t)kvh * P.C.head_stride + col;
+          Far f = {-2, 0};                              // -2: before the sequence
+          if (j >= 0 && k < m1) {
+            const int page = P.C.by_page.over((int)j);
+            f.slot = (int)j - page * P.C.page_size;
+            f.id = page < P.B.table_stride ? __ldg(table + page) : -1;
+          }
+          return f;
+        };
+        Far next = look(m0);
+        for (int k = m0; k < m1; ++k) {
+          const Far now = next;
+          next = look(k + 1);
+          const bool exists = now.id >= 0 && now.id < P.C.num_pages;
+          if (now.id != -2 && !exists) g_bad_page = 1;
+          const int64_t at = exists ? (int64_t)now.id * P.C.page_stride + (int64_t)now.slot * P.C.token_stride + (int64_t)kvh * P.C.head_stride + col : 0;
           Half<HALF / 2> kk, vv;
-          half_row(kk, P.C.K + at, sl.exists);
-          half_row(vv, P.C.V + at, sl.exists);
+          half_row(kk, P.C.K + at, exists);
+          half_row(vv, P.C.V + at, exists);
           const float d = half_dot(mine, kk);          // every lane: it has a shuffle
-          const float x = sl.exists ? d * P.scale_log2 : -INFINITY;
+          const float x = exists ? d * P.scale_log2 : -INFINITY;
           const bool up = x > fm + LAZY;
           if (__any_sync(0xffffffffu, up)) {
             const float c = up ? ex2(fm - x) : 1.f;
@@ -449,7 +459,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll
             for (int e = 0; e < HALF; ++e) acc[e] *= c;
           }
-          const float w = sl.exists ? ex2(x - mst_paged::reference(fm)) : 0.f;
+          const float w = exists ? ex2(x - mst_paged::reference(fm)) : 0.f;
           fs += w;
           uint16_t wb, dummy;
           halves(pack_bf16(w, 0.f), wb, dummy);
@@ -494,12 +504,27 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
         uint32_t w[32];
         if ((there[0] | there[1]) && i_hi >= k0 && (MODE == DENSE || i_lo - (k0 + 63) <= P.l)) {      // some pair may be attended
           const bool some_not = MODE == DENSE || (there[0] & there[1]) != ~0u || i_lo < k0 + 63 || i_hi - k0 > P.l;   // some pair may not be
-          auto mask = [&](uint32_t (&x)[16], int g) {
-            if (!some_not) return;
+          uint32_t seen[2] = {there[0], there[1]};      // this row's keys
+          if (some_not) {
+            if (MODE == DENSE) {
+#pragma unroll 1
+              for (int e = 0; e < 64; ++e)
+                if (!near_sees(P.l, pos, k0 + e)) seen[e >> 5] &= ~(1u << (e & 31));
+            } else {
+              const int last = pos - k0, first = last < 0 ? 0 : last - P.l;     // keys first .. last of the 64
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const bool sees = MODE == DENSE ? near_sees(P.l, pos, k0 + 16 * g + e) : (unsigned)(pos - k0 - 16 * g - e) <= (unsigned)P.l;
-              if (!((there[g >> 1] >> (16 * (g & 1) + e)) & 1u) || !sees) x[e] = 0xFF800000u;   // -inf
+              for (int g = 0; g < 2; ++g) {
+                const int hi = last - 32 * g, lo = first - 32 * g;
+                seen[g] &= hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1u;
+                seen[g] &= lo <= 0 ? ~0u : lo > 31 ? 0u : ~0u << lo;
+              }
+            }
+          }
+          auto mask = [&](uint32_t (&x)[8], int g) {
+            if (some_not) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (!((seen[g >> 2] >> (8 * (g & 3) + e)) & 1u)) x[e] = 0xFF800000u;   // -inf
             }
           };
           // Weights against the reference as it is.  Their sum tells whether a score lies too far above it, which is seldom, so nobody looks for the
@@ -509,33 +534,33 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           for (int pass = 0;; ++pass) {
             const float nm = -mst_paged::reference(m);
             float add[4] = {0.f, 0.f, 0.f, 0.f};
-            uint32_t x[2][16];
-            tmem_ld16_nowait(t_s, x[0]);
+            uint32_t x[2][8];
+            tmem_ld8_nowait(t_s, x[0]);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              tmem_ld16_wait(x[g & 1]);
-              if (g < 3) tmem_ld16_nowait(t_s + 16u * (g + 1), x[(g + 1) & 1]);
+            for (int g = 0; g < 8; ++g) {
+              tmem_ld8_wait(x[g & 1]);
+              if (g < 7) tmem_ld8_nowait(t_s + 8u * (g + 1), x[(g + 1) & 1]);
               mask(x[g & 1], g);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
+              for (int e = 0; e < 4; ++e) {
                 const float lo = ex2(fmaf(__uint_as_float(x[g & 1][2 * e]), P.scale_log2, nm));
                 const float hi = ex2(fmaf(__uint_as_float(x[g & 1][2 * e + 1]), P.scale_log2, nm));
                 add[e & 1] += lo;
                 add[2 + (e & 1)] += hi;
-                w[8 * g + e] = pack_bf16(lo, hi);
+                w[4 * g + e] = pack_bf16(lo, hi);
               }
             }
             sum = (add[0] + add[1]) + (add[2] + add[3]);
             if (pass == 1 || !__any_sync(0xffffffffu, sum > MOST || (live && m == -INFINITY))) break;
             float top = -INFINITY;
 #pragma unroll 1
-            for (int g = 0; g < 4; ++g) {
-              uint32_t x[16];
-              tmem_ld16_nowait(t_s + 16u * g, x);
-              tmem_ld16_wait(x);
+            for (int g = 0; g < 8; ++g) {
+              uint32_t x[8];
+              tmem_ld8_nowait(t_s + 8u * g, x);
+              tmem_ld8_wait(x);
               mask(x, g);
 #pragma unroll
-              for (int e = 0; e < 16; ++e) top = fmaxf(top, __uint_as_float(x[e]));
+              for (int e = 0; e < 8; ++e) top = fmaxf(top, __uint_as_float(x[e]));
             }
             top *= P.scale_log2;
             const bool up = top > m && (sum > MOST || m == -INFINITY);
