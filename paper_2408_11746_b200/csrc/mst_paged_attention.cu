@@ -383,34 +383,44 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
 }
 
 // ---------------------------------------------------------------------------------------------- the call
-constexpr int TILE_ROWS = 128, TILES_FROM = 33;
+// Which form, by what the few-row form would go through: entries of its lists, over all 16-row tiles.  Up to 16 rows it always serves (12 heads, 3000
+// positions, 16 new tokens of 32 sequences 70 us, in 128-row tiles 86); beyond, a list that fills eight such tiles is better walked once.  Measured with 24 to
+// 96 new tokens of 1, 8 and 32 sequences, few rows / tiles in us: every position attended 13.5 / 22 (72 thousand entries), 15 / 23 (144), 22 / 24 (216),
+// 38 / 29 (576), 88 / 86 (2304); stride 256, where tiles form a strided key for each row, 13 / 22 (86), 25 / 35 (257), 50 / 64 (515), 69 / 75 (686),
+// 94 / 81 (1030); 4 x 512 tokens over 8192, stride 256 78 / 85 (1178), stride 1024 89 / 65 (1768), 4 x 2048 tokens, stride 256 255 / 160 (4712).
+// (A few-row form of 32 rows lost to the one of 16 in all of them.)
+constexpr int TILE_ROWS = 128, FEW_ROWS = 16;
+constexpr double TILES_FROM = 250e3, TILES_FROM_STRIDED = 900e3;
 Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, int stride) {
   Plan p;
   const int group = heads / c.kv_heads;
-  const int64_t rows = (int64_t)(b.max_new > 0 ? b.max_new : 1) * group, len = b.max_len > 0 ? b.max_len : 1;
+  const int64_t new_tokens = b.max_new > 0 ? b.max_new : 1, rows = new_tokens * group, len = b.max_len > 0 ? b.max_len : 1;
   const int64_t lists = (int64_t)(b.batch > 0 ? b.batch : 1) * c.kv_heads;
-  p.tiles = rows >= TILES_FROM && group <= TILE_ROWS && (int64_t)c.kv_heads * 64 < 0x7FFFFFFF;
-  p.rows = p.tiles ? TILE_ROWS / group * group : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-  const int64_t tiles = (rows + p.rows - 1) / p.rows, most = 65535;
-  p.count = (int)(tiles < most ? tiles : most);
-  // units of the longest list: 64 entries; or tiles of 128 keys and strided keys, which take about as long
-  const int64_t in_tile = (p.rows + group - 1) / group, nt = b.max_new < in_tile ? (b.max_new > 0 ? b.max_new : 1) : in_tile;
-  int64_t units;
-  int waves;      // of blocks, two of which an SM holds, that ranges are cut for
-  p.least = 8;
+  // entries of the longest list of a tile of `r` rows
+  auto entries = [&](int r) {
+    const int64_t in_tile = (r + group - 1) / group, nt = new_tokens < in_tile ? new_tokens : in_tile;
+    return stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
+  };
+  const bool strided = len / 2 >= stride && stride >= DENSE_BELOW;
+  p.tiles = rows > FEW_ROWS && group <= TILE_ROWS &&
+            (double)lists * (double)((rows + FEW_ROWS - 1) / FEW_ROWS) * (double)entries(FEW_ROWS) >= (strided ? TILES_FROM_STRIDED : TILES_FROM);
+  p.rows = p.tiles ? TILE_ROWS / group * group : rows <= FEW_ROWS / 2 ? FEW_ROWS / 2 : FEW_ROWS;
+  const int64_t tiles = (rows + p.rows - 1) / p.rows;
+  p.count = (int)(tiles < 65535 ? tiles : 65535);
+  // Long lists are cut into ranges until there are blocks for the whole GPU, two of which an SM holds.  Tiles: for one wave and no more (432 blocks of up to
+  // 94 tiles 272 us, cut into 960 281 us).  Few rows: for two, as lists are of many lengths (long ragged contexts 41.8 us, for six waves 47.9).
+  // units: tiles of 128 keys and strided keys, which take about as long; or 64 entries
+  int64_t units, want = 2 * (int64_t)mst_sm_count();
   if (p.tiles) {
-    const bool dense = stride < DENSE_BELOW;
-    const int64_t near = (dense || stride + nt > len ? len : stride + nt) / KEYS_OF_TILE + 1, far = dense ? 0 : len / stride;
-    units = near + far;
-    waves = 1;
+    const int64_t nt = TILE_ROWS / group;
+    units = (stride < DENSE_BELOW || stride + nt > len ? len : stride + nt) / KEYS_OF_TILE + 1 + (strided ? len / stride : 0);
   } else {
-    const int64_t list = stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
-    units = (list + UNIT - 1) / UNIT;
-    waves = 2;
+    units = (entries(p.rows) + UNIT - 1) / UNIT;
+    want *= 2;
   }
-  const int64_t blocks = lists * tiles, want = 2 * waves * (int64_t)mst_sm_count();
+  p.least = 8;      // 512 entries: a second launch costs as long as they take
+  const int64_t blocks = lists * tiles, fit = (units + p.least - 1) / p.least;
   int64_t splits = p.tiles ? want / blocks : (want + blocks - 1) / blocks;
-  const int64_t fit = (units + p.least - 1) / p.least;
   if (splits > fit) splits = fit;
   if (splits > 64) splits = 64;
   if (splits < 1) splits = 1;
@@ -434,7 +444,7 @@ mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
 }
 template <int D>
 mst_status_t launch_rows(const Params& P, const Plan& plan, cudaStream_t s) {
-  return plan.rows == 8 ? launch_rows<D, 1>(P, plan, s) : plan.rows == 16 ? launch_rows<D, 2>(P, plan, s) : launch_rows<D, 4>(P, plan, s);
+  return plan.rows == FEW_ROWS / 2 ? launch_rows<D, 1>(P, plan, s) : launch_rows<D, 2>(P, plan, s);
 }
 template <int D>
 mst_status_t launch_join(const Params& P, const Plan& plan, cudaStream_t s) {
@@ -494,6 +504,7 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   const size_t need = workspace_of(*cache, *batch, heads, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return MST_ERR_CAPACITY;
   if (batch->batch == 0 || batch->tokens == 0) return MST_OK;
+  if (need > 0 && ((int64_t)batch->tokens * heads + 3) / 4 > 0x7FFFFFFF) return MST_ERR_SHAPE;
   MST_TRY(mst_on_this_device({Q, Out, lse, need ? workspace : nullptr, P.C.K, P.C.V, P.B.first, P.B.len, P.B.table}));
   P.Q = (const __nv_bfloat16*)Q;
   P.Out = (__nv_bfloat16*)Out;

@@ -86,11 +86,18 @@ class Case:
             assert (np.abs(zz[:, :n][~empty] - ref_z[:, :n][~empty]) <= 2e-4).all()
             assert (zz[:, n:] == 7.0).all()
 
+    def said(self, form):
+        """What the call is told of its sizes, which decides the kernel and how the work is cut up and nothing else: "few" rows, 128-row "tiles",
+        "ranges" of tiles (two or three from 1024 positions, or from 48 tiles and strided keys on), or as things are."""
+        self.batch.max_new, self.batch.max_len = {"few": (1, self.max_len), "tiles": (4096, 1 << 20), "ranges": (700, 3000), "far": (4000, 6000),
+                                                  "true": (self.max_new, self.max_len)}[form]
+        return self
+
     def run(self, stride, pad=0):
         self.upload()
-        out, z = self.attend(stride, pad)
-        self.check(stride, out, z)
-        return out, z
+        for form in ("true", "few", "tiles", "ranges", "far"):
+            out, z = self.said(form).attend(stride, pad)
+            self.check(stride, out, z)
 
 
 # new tokens and lengths: one token each; drafts; chunks; nothing new; nothing at all; a length that is its new tokens
@@ -143,9 +150,10 @@ def test_pages_that_do_not_exist(new, stride):
     c = Case([new, new], [500, 420], 2, 2, page=16)
     c.table[0, 3], c.table[0, 31], c.table[1, 10], c.table[1, 0] = -1, 10 ** 6, -(1 << 31), c.K.shape[0]
     c.upload()
-    out, z = c.attend(stride)
-    c.check(stride, out, z, flags=BAD_PAGE)
-    assert mst.mst_device_error_flags() == 0
+    for form in ("few", "tiles"):
+        out, z = c.said(form).attend(stride)
+        c.check(stride, out, z, flags=BAD_PAGE)
+        assert mst.mst_device_error_flags() == 0
 
 
 @pytest.mark.parametrize("stride", [FAR, 64, 170])
@@ -154,14 +162,16 @@ def test_a_table_shorter_than_the_length(new, stride):
     c = Case([new], [400], 2, 2, page=16)
     c.table = c.table[:, :20].contiguous()
     c.upload()
-    out, z = c.attend(stride)
-    c.check(stride, out, z, flags=BAD_PAGE)
+    for form in ("few", "tiles"):
+        out, z = c.said(form).attend(stride)
+        c.check(stride, out, z, flags=BAD_PAGE)
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("stride", [FAR, 64])
+@pytest.mark.parametrize("form", ["few", "tiles"])
 @pytest.mark.parametrize("new,page", [([1, 6], 16), ([96, 200], 64), ([33, 70], 7)])
-def test_what_is_not_attended_does_not_reach_a_result(new, page, stride, value):
+def test_what_is_not_attended_does_not_reach_a_result(new, page, stride, value, form):
     # the last token's key and value are no numbers, nor is what the pages hold behind the lengths, nor a page of nobody; rows before it do not see them
     c = Case(new, [300, 420], 4, 2, page=page)
     K, V = c.K.clone(), c.V.clone()
@@ -176,7 +186,7 @@ def test_what_is_not_attended_does_not_reach_a_result(new, page, stride, value):
     c.K[at] = value
     c.V[at] = value
     c.upload()
-    out, z = c.attend(stride)
+    out, z = c.said(form).attend(stride)
     assert mst.mst_device_error_flags() == 0
     keep = host(out)[: c.rows - 1]
     assert np.isfinite(keep).all()
@@ -197,14 +207,14 @@ def test_what_is_not_attended_does_not_reach_a_result(new, page, stride, value):
 def test_peaked_rows(new):
     c = Case([new, new], [900, 300], 2, 2, std=4.0)       # scores of variance 256: a few keys have all the weight
     c.upload()
-    out, z = c.attend(FAR)
+    out, z = c.said("tiles" if new == 100 else "few").attend(FAR)
     # scores up to about 100: their rounding (2^-24 of sum |q k| / 8, some 300) and that of the exponents at 2^7 are below 4e-5 each
     c.check(FAR, out, z)
 
 
 def test_no_lse_and_repeats():
-    for new, length in (([1, 1], [5000, 300]), ([100, 300], [2000, 300])):
-        c = Case(new, length, 4, 2).upload()
+    for new, length, form in (([1, 1], [5000, 300], "true"), ([100, 300], [2000, 300], "true"), ([100, 300], [2000, 300], "tiles"), ([100, 300], [6000, 300], "far")):
+        c = Case(new, length, 4, 2).upload().said(form)
         a, z = c.attend(128)
         for _ in range(3):
             b, y = c.attend(128)
@@ -242,11 +252,12 @@ def test_offsets_beyond_32_bits():
         c.cache = mst.PagedCache(K, V)
         c.batch = mst.PagedBatch(c.dev_first, c.dev_len, c.dev_table, c.tokens, c.max_new, c.max_len)
         for stride in (FAR, 64):
-            c.check(stride, *c.attend(stride))
+            for form in ("few", "tiles"):
+                c.check(stride, *c.said(form).attend(stride))
 
 
 def test_streams_and_captured_graphs_side_by_side():
-    a, b = Case([1, 1], [5000, 700], 4, 2, seed=1).upload(), Case([90, 40], [1500, 800], 4, 2, seed=2).upload()
+    a, b = Case([1, 1], [5000, 700], 4, 2, seed=1).upload(), Case([90, 40], [1500, 800], 4, 2, seed=2).upload().said("tiles")
     want = [a.attend(128), b.attend(128)]
     graphs, outs, keep = [], [], []
     for c in (a, b):
@@ -401,7 +412,8 @@ def test_generation_agrees_with_the_training_time_attention(stride):
         at = [a + s for a, s in zip(at, step)]
         first = torch.tensor([0, step[0], sum(step)], dtype=torch.int32, device=dev())
         length = torch.tensor(at, dtype=torch.int32, device=dev())
-        batch = mst.PagedBatch(first, length, table, sum(step), max(step), max(at))
+        many = max(step) > 100                       # the prompts' chunks in tiles
+        batch = mst.PagedBatch(first, length, table, sum(step), 4096 if many else max(step), 1 << 20 if many else max(at))
         q = torch.empty(max(sum(step), 1), C, dtype=torch.bfloat16, device=dev())
         o, zz = torch.empty_like(q), torch.empty(H, max(sum(step), 1), device=dev())
         p = new.data_ptr()
