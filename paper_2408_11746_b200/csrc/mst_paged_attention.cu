@@ -298,8 +298,8 @@ __global__ void __launch_bounds__(32 * RW, 2) paged_rows_kernel(const __grid_con
       if (__any_sync(0xffffffffu, bad)) {
         const uint32_t w_lo = lo < T.W ? lo : T.W, w_hi = hi < T.W ? hi : T.W, f_lo = lo - w_lo, f_hi = hi - w_hi;   // of the window, behind it
         const uint32_t t_in = (uint32_t)(t - T.t_lo), nt = (uint32_t)T.nt;
-        row_again<D>(P, b, (int)token, h, T.p_lo + (int)t_in, T.w0 + (int)w_lo, T.w0 + (int)w_hi, T.l - 1, T.dense, 1 + (int)steps_below(f_lo, t_in, nt),
-                     1 + (int)steps_below(f_hi, t_in, nt), o, mm, total_w);
+        row_again<D>(P, b, (int)token, h, T.p_lo + (int)t_in, T.w0 + (int)w_lo, T.w0 + (int)w_hi, T.l - 1, T.dense,
+                     T.m0 + (int)steps_below(f_lo, t_in, nt), T.m0 + (int)steps_below(f_hi, t_in, nt), o, mm, total_w);
       }
       if (active == 1) {
         finish<E>(P, token, h, lane, o, mm, total_w);

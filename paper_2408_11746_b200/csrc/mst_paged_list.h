@@ -4,7 +4,8 @@
 // A tile is up to R neighbours among one sequence's (new token, query head of one key head) pairs, so that the heads of a group share keys.
 // Its keys are a list: the window of all its tokens, positions w0 .. w0 + W - 1 in order; then for each m >= 1 the positions m l behind each of its
 // tokens, which only that token's rows look at.  Where a tile has l tokens or more the window is everything from 0 on and the set is left to
-// the mask.  Lists have below 2^32 entries for any lengths: the window ends at the last position and the rest has fewer than that.
+// the mask.  Whatever a length says, next to nothing is listed that lies at `reach` or beyond, where the table has no room for a position: the table bounds
+// the work, and lists stay below 2^32 entries.
 #pragma once
 #include <stdint.h>
 
@@ -46,6 +47,7 @@ struct List {
   int t_lo, nt;           // the tokens it touches
   int p_lo, p_hi;         // their positions
   int l, w0;
+  int m0;                 // the first m: 1, or what brings the tile's first token below reach
   uint32_t W, N;          // entries of the window, of the list
   bool dense;
 
@@ -70,7 +72,8 @@ struct List {
     const int64_t w = dense ? 0 : (int64_t)p_lo - l + 1;
     w0 = w > 0 ? (int)w : 0;
     W = last >= w0 ? (uint32_t)(last - w0 + 1) : 0u;
-    N = W + (dense || p_hi < l ? 0u : (uint32_t)stride.over(p_hi) * (uint32_t)nt);
+    m0 = p_lo >= reach && p_lo - reach >= l ? stride.over((int)(p_lo - reach)) : 1;
+    N = W + (dense || p_hi < l ? 0u : (uint32_t)(stride.over(p_hi) - m0 + 1) * (uint32_t)nt);
     return true;
   }
   MST_HD Key key(uint32_t n) const {
@@ -83,7 +86,7 @@ struct List {
       m = f / (uint32_t)nt;
       who = (int)(f - m * (uint32_t)nt);
     }
-    const int64_t p = (int64_t)p_lo + who - (int64_t)(m + 1) * l;
+    const int64_t p = (int64_t)p_lo + who - ((int64_t)m + m0) * l;
     return Key{p < 0 ? -1 : (int)p, who};
   }
   // does the row of the tile's token `t`, at position p, look at an entry
@@ -120,14 +123,15 @@ struct List {
 // tile at least.
 constexpr int KEYS_OF_TILE = 128, DENSE_BELOW = 64;
 struct TileWalk {
-  int first, near, far;
+  int first, near, far, m_first;
   MST_HD TileWalk(const List& T, int64_t reach) {
     const bool dense = T.l < DENSE_BELOW;
     const int64_t from = dense || (int64_t)T.p_lo - T.l < 0 ? 0 : (int64_t)T.p_lo - T.l;
     const int64_t last = T.p_hi < reach ? T.p_hi : reach - 1;
     first = (int)(from / KEYS_OF_TILE) * KEYS_OF_TILE;
     near = T.p_hi < 0 ? 0 : last >= first ? (int)((last - first) / KEYS_OF_TILE) + 1 : 1;
-    far = dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - 1;
+    m_first = T.m0 > 2 ? T.m0 : 2;
+    far = dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - m_first + 1;
   }
   // Range `split` of at most `splits` equal ranges, each with `least` tiles and steps or more and a near tile: near tiles n0 .. n1 - 1, strided keys
   // m0 .. m1 - 1 steps behind.  active: how many ranges there are.
@@ -139,8 +143,8 @@ struct TileWalk {
     if (split >= active) return false;
     n0 = (int)((int64_t)near * split / active);
     n1 = (int)((int64_t)near * (split + 1) / active);
-    m0 = 2 + (int)((int64_t)far * split / active);
-    m1 = 2 + (int)((int64_t)far * (split + 1) / active);
+    m0 = m_first + (int)((int64_t)far * split / active);
+    m1 = m_first + (int)((int64_t)far * (split + 1) / active);
     return true;
   }
 };

@@ -212,6 +212,40 @@ def test_peaked_rows(new):
     c.check(FAR, out, z)
 
 
+def test_lengths_and_rows_that_make_no_sense():
+    # far beyond the table, below zero, rows that overlap, go backwards or lie outside: the sequence in between is served, nothing outside is written
+    c = Case([1, 3, 40], [50, 60, 300], 2, 2)
+    for form in ("few", "tiles"):
+        for stride in (FAR, 64, 7):
+            c.upload().said(form)
+            c.dev_len.copy_(torch.tensor([(1 << 31) - 1, -(1 << 31), 300], dtype=torch.int32))
+            out, z = c.attend(stride)
+            assert mst.mst_device_error_flags() == BAD_PAGE
+            ref, ref_z, weight = paged.paged_attention(c.Q.float().numpy().reshape(c.tokens, 2, 64), c.K.float().numpy(), c.V.float().numpy(), [0, 0, 4, 44],
+                                                       [0, 0, 300], c.table.numpy(), stride)
+            o = host(out).reshape(ref.shape)
+            assert (np.abs(o[4:] - ref[4:]) <= 2.0 ** -8 * np.abs(ref[4:]) + (2.0 ** -8 + 4e-4) * weight[4:]).all()
+            assert (o[1:4] == 0).all() and np.isneginf(host(z)[:, 1:4]).all()
+            c.dev_first.copy_(torch.tensor([-7, 1 << 30, 4, 3], dtype=torch.int32))
+            out, z = c.attend(stride)
+            assert (host(out) == 7.0).all() and (host(z) == 7.0).all()
+            mst.mst_device_error_flags()
+
+
+@pytest.mark.parametrize("new,length,max_new,max_len,stride,kernel", [
+    ([1, 1], [3000, 200], 1, 3000, FAR, "paged_rows_kernel"), ([16], [5000], 16, 5000, 64, "paged_rows_kernel"),
+    ([200, 200], [900, 900], 200, 900, FAR, "paged_rows_kernel"), ([800, 200], [2000, 900], 800, 2000, FAR, "paged_tiles_kernel"),
+    ([800, 200], [2000, 900], 800, 20000, 64, "paged_tiles_kernel")])
+def test_kernel_of_a_call(new, length, max_new, max_len, stride, kernel):
+    from torch.profiler import ProfilerActivity, profile
+    c = Case(new, length, 4, 2, max_new=max_new, max_len=max_len).upload()
+    c.attend(stride)
+    with profile(activities=[ProfilerActivity.CUDA]) as seen:
+        c.attend(stride)
+    names = [e.name for e in seen.events() if "paged_" in e.name and "join" not in e.name]
+    assert len(names) == 1 and kernel in names[0], names
+
+
 def test_no_lse_and_repeats():
     for new, length, form in (([1, 1], [5000, 300], "true"), ([100, 300], [2000, 300], "true"), ([100, 300], [2000, 300], "tiles"), ([100, 300], [6000, 300], "far")):
         c = Case(new, length, 4, 2).upload().said(form)

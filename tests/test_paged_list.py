@@ -116,16 +116,28 @@ def test_tiles_of_lengths_that_make_no_sense(lib, length, stride, reach):
     assert lib.walk_of(*_args(0, 300, length, 1, stride, reach, 1, 128), 16, 4, 0, out) == 1
     first, near, far, n0, n1, m0, m1, active = list(out)
     assert first >= 0 and first % TILE == 0 and 0 <= near <= (1 << 31) // TILE and far >= 0 and 1 <= active <= 16 and (near > 0) == (length > 300 - 128 - 128)
-    assert first + TILE * near <= max(length, 0) + TILE
+    assert first + TILE * near <= max(length, 0) + TILE and far <= reach // stride + 3
     if reach < length:
         assert near <= max(1, reach // TILE + 1)
 
 
-def test_rows_stay_within_the_table(lib):
-    got = _seen_by_rows(lib, 4, 100, 1, 64, 16, 2, 1, reach=80)
-    for r, seen in got.items():
-        i = 96 + r
-        assert set(seen) >= {j for j in range(80) if 0 <= i - j < 64}
+@pytest.mark.parametrize("stride", [1 << 30, 64, 100, 7, 3])
+@pytest.mark.parametrize("reach", [0, 1, 80, 128, 333, 400])
+@pytest.mark.parametrize("R", [16, 128])
+def test_rows_of_a_table_that_is_too_short(lib, stride, reach, R):
+    """Positions from `reach` on need not be listed; all the others are, once."""
+    n, length = 40, 400
+    got = _seen_by_rows(lib, n, length, 1, stride, R, 3, 1, reach=reach)
+    out = (ctypes.c_int32 * 8)()
+    for r in range(n):
+        i = length - n + r
+        want = [j for j in range(min(i + 1, reach)) if i - j < stride or (i - j) % stride == 0]
+        assert sorted(j for j in got[r] if j < reach) == want
+        args = _args(5, n, length, 1, stride, reach, r // R, R)
+        assert lib.walk_of(*args, 1, 8, 0, out) == 1
+        first, near, far, n0, n1, m0, m1, active = list(out)
+        seen = [k for k in range(first, first + TILE * near) if k < reach and lib.near(*args, i, k)] + [i - m * stride for m in range(m0, m1)]
+        assert sorted(j for j in seen if 0 <= j < reach) == want
 
 
 @pytest.mark.parametrize("first,end,tokens", [(0, 0, 10), (5, 4, 10), (-1, 3, 10), (4, 11, 10), (-(1 << 31), (1 << 31) - 1, 10)])
@@ -140,7 +152,7 @@ def test_rows_that_are_not_there(lib, first, end, tokens):
 def test_lengths_that_make_no_sense(lib, length, stride, reach):
     args = _args(0, 33, length, 1, stride, reach, 1, 16)
     row0, rows, t_lo, nt, p_lo, p_hi, W, N, dense = _tile(lib, args)
-    assert 0 <= W <= N < 1 << 32 and W <= max(0, reach)
+    assert 0 <= W <= N < 1 << 32 and W <= max(0, reach) and N - W <= (reach // stride + 3) * nt
     if length <= 0:
         assert N == 0
     lha = (ctypes.c_int64 * 3)()
