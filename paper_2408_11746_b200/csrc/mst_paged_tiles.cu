@@ -11,7 +11,10 @@
 //              written it over the scores.
 // Tensor memory: the halves' scores in columns 0-63 and 64-127, their outputs behind: two blocks an SM at head_dim 64.  Ranges of a list (blockIdx.x)
 // leave sums for the join.
-// Bound: exponentials (16 a clock and SM: 1024 clocks for 128 x 128, the products need 640).
+// Bound: the chain of a half through products, exponentials and barriers, four of which an SM has at a time: 3050 clocks a 128 x 128 tile and block,
+// where the exponential unit (16 a clock) needs 1024 for each of the two blocks and the products 640.  4479 tokens of three sequences over 4000 to 12000
+// positions, 12 heads: 272 us, exponential unit 54 % busy.  (Tiles of 64 keys with two score buffers 305 us, tiles of 128 without independent halves
+// 304, one lane that issues by itself 5 us more.)
 #include <cuda.h>
 
 #include <type_traits>
@@ -321,8 +324,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else if (warp == CW + 1) {
       // ------------------------------------------------------------------------------------------ products
       // The whole warp goes through the loop and one elected lane issues.  What the instructions name is the same in every turn, a slot's and a half's
-      // part being constants, and stays in uniform registers (by a lane of its own, with addresses worked out on the way, a tile's instructions took
-      // 1300 clocks to issue).
+      // part being constants, and there is no branch around them: a tile's sixteen products take 1000 clocks to issue (1300 in a branch of a lane).
       const uint32_t leader = elect_one();
       const uint64_t qd = smem_desc(own, 16, 1024), kd0 = smem_desc(ring_k, 16, 1024), vd0 = smem_desc(ring_v, 16, 1024);
       constexpr uint64_t step = S::SLOT_BYTES >> 4, part = (2 * TILE_BYTES) >> 4, half_tile = TILE_BYTES >> 4;
