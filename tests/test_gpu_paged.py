@@ -88,14 +88,15 @@ class Case:
 
     def said(self, form):
         """What the call is told of its sizes, which decides the kernel and how the work is cut up and nothing else: "few" rows, 128-row "tiles",
-        "ranges" of tiles (two or three from 1024 positions, or from 48 tiles and strided keys on), or as things are."""
-        self.batch.max_new, self.batch.max_len = {"few": (1, self.max_len), "tiles": (4096, 1 << 20), "ranges": (700, 3000), "far": (4000, 6000),
+        "ranges" of tiles (two or three from 1024 positions, or from 48 tiles and strided keys on), tiles of which a block sees to one after "again"
+        another, or as things are."""
+        self.batch.max_new, self.batch.max_len = {"few": (1, self.max_len), "tiles": (4096, 1 << 20), "ranges": (700, 3000), "far": (4000, 6000), "again": (40, 1 << 20),
                                                   "true": (self.max_new, self.max_len)}[form]
         return self
 
     def run(self, stride, pad=0):
         self.upload()
-        for form in ("true", "few", "tiles", "ranges", "far"):
+        for form in ("true", "few", "tiles", "ranges", "far", "again"):
             out, z = self.said(form).attend(stride, pad)
             self.check(stride, out, z)
 
@@ -230,20 +231,6 @@ def test_lengths_and_rows_that_make_no_sense():
             out, z = c.attend(stride)
             assert (host(out) == 7.0).all() and (host(z) == 7.0).all()
             mst.mst_device_error_flags()
-
-
-@pytest.mark.parametrize("new,length,max_new,max_len,stride,kernel", [
-    ([1, 1], [3000, 200], 1, 3000, FAR, "paged_rows_kernel"), ([16], [5000], 16, 5000, 64, "paged_rows_kernel"),
-    ([200, 200], [900, 900], 200, 900, FAR, "paged_rows_kernel"), ([800, 200], [2000, 900], 800, 2000, FAR, "paged_tiles_kernel"),
-    ([800, 200], [2000, 900], 800, 20000, 64, "paged_tiles_kernel")])
-def test_kernel_of_a_call(new, length, max_new, max_len, stride, kernel):
-    from torch.profiler import ProfilerActivity, profile
-    c = Case(new, length, 4, 2, max_new=max_new, max_len=max_len).upload()
-    c.attend(stride)
-    with profile(activities=[ProfilerActivity.CUDA]) as seen:
-        c.attend(stride)
-    names = [e.name for e in seen.events() if "paged_" in e.name and "join" not in e.name]
-    assert len(names) == 1 and kernel in names[0], names
 
 
 def test_no_lse_and_repeats():

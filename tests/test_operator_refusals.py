@@ -152,6 +152,19 @@ def test_attention_head_dims_and_workspaces(mst):
     assert mst.mst_paged_attention_workspace(_cache(mst), long, 2, 1) == need
 
 
+@pytest.mark.parametrize("max_new,max_len,stride,splits", [
+    (1, 3000, 1 << 30, 6),          # few rows: 4 lists of 47 units of 64 entries, eight of them at least to a range
+    (800, 20000, 1 << 30, 5),       # tiles: 52 blocks, for one wave of 296 (few rows: 400 blocks, two ranges)
+    (200, 900, 1 << 30, 2),         # few rows: 4 lists of 25 tiles, 90 thousand entries
+    (800, 20000, 64, 5),            # tiles again: 1.0 million entries
+    (800, 4000, 64, 2),             # few rows: 0.3 million
+    (4096, 1 << 20, 1 << 30, 1)])   # tiles: a wave of blocks as it is
+def test_forms_of_the_attention(mst, max_new, max_len, stride, splits):
+    """Kernel and ranges follow from what is said of the sizes; the workspace tells how many ranges there may be (148 SMs)."""
+    n = mst.mst_paged_attention_workspace(_cache(mst), _batch(mst, tokens=1000, max_new=max_new, max_len=max_len), 4, stride)
+    assert n == (splits * 1000 * 4 * 66 * 4 if splits > 1 else 0)
+
+
 def test_calls_without_sequences(mst):
     none = _batch(mst, batch=0, first=None, len=None, page_table=None)
     _append(mst, batch=none)
