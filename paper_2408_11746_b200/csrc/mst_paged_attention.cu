@@ -391,8 +391,6 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
 // 38 / 29 (576), 88 / 86 (2304); stride 256, where tiles form a strided key for each row, 13 / 22 (86), 25 / 35 (257), 50 / 64 (515), 69 / 75 (686),
 // 94 / 81 (1030); 4 x 512 tokens over 8192, stride 256 78 / 85 (1178), stride 1024 89 / 65 (1768), 4 x 2048 tokens, stride 256 255 / 160 (4712).
 // (A few-row form of 32 rows lost to the one of 16 in all of them.)
-// room for (sequence, tile of rows) entries
-int64_t even_most(const mst_paged_batch_t& b, int group, int rows) { return ((int64_t)b.tokens * group) / rows + b.batch; }
 constexpr int TILE_ROWS = 128, FEW_ROWS = 16;
 constexpr double TILES_FROM = 250e3, TILES_FROM_STRIDED = 900e3;
 Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, int stride) {
@@ -431,20 +429,11 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   const int64_t each = (units + splits - 1) / splits;
   if (each > p.least) p.least = (int)(each < 0x7FFFFFFF ? each : 0x7FFFFFFF);
   p.splits = (int)splits;
-  // more blocks than run at once, and no strided keys in any length that the table has room for: even parts
-  const int64_t reach = (int64_t)b.table_stride * c.page_size;
-  p.even = p.tiles && (reach / 2 < stride || stride < DENSE_BELOW) && blocks > even_blocks(c.head_dim) && even_most(b, group, p.rows) < (1 << 28);
-  if (p.even) p.splits = 1;
   return p;
 }
-// bytes of an even call's entries, a multiple of 16
-size_t even_bytes(const mst_paged_batch_t& b, int64_t most) {
-  return (8 * (size_t)(most + 1) + 8 * (size_t)most + 4 * ((size_t)b.batch + 1) + 15) & ~(size_t)15;
-}
 size_t workspace_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, const Plan& p) {
-  const size_t row = (size_t)(c.head_dim + 2) * sizeof(float);
-  if (p.even) return even_bytes(b, even_most(b, heads / c.kv_heads, p.rows)) + (size_t)even_blocks(c.head_dim) * 2 * TILE_ROWS * row;
-  return p.splits <= 1 ? 0 : (size_t)p.splits * (size_t)b.tokens * (size_t)heads * row;
+  if (p.splits <= 1) return 0;
+  return (size_t)p.splits * (size_t)b.tokens * (size_t)heads * (size_t)(c.head_dim + 2) * sizeof(float);
 }
 
 template <int D, int NT>
@@ -534,19 +523,7 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
   P.by_l = Divider::of((uint32_t)stride);
   P.by_least = Divider::of((uint32_t)plan.least);
   P.part_o = (float*)workspace;
-  if (plan.even) {
-    const int64_t most = even_most(*batch, P.group, plan.rows);
-    P.even.prefix = (int64_t*)workspace;
-    P.even.entry = (int2*)(P.even.prefix + most + 1);
-    P.even.first = (int32_t*)(P.even.entry + most);
-    P.even.most = (int)most;
-    P.even.blocks = even_blocks(cache->head_dim);
-    P.even.rows = plan.rows;
-    P.part_o = (float*)((unsigned char*)workspace + even_bytes(*batch, most));
-    P.part_m = P.part_o + (size_t)P.even.blocks * 2 * TILE_ROWS * (size_t)cache->head_dim;
-  } else if (need) {
-    P.part_m = P.part_o + (size_t)plan.splits * (size_t)batch->tokens * (size_t)heads * (size_t)cache->head_dim;
-  }
+  if (need) P.part_m = P.part_o + (size_t)plan.splits * (size_t)batch->tokens * (size_t)heads * (size_t)cache->head_dim;
   cudaStream_t s = (cudaStream_t)stream;
   if (plan.tiles) MST_TRY(launch_tiles(P, plan, s));
   else MST_TRY(cache->head_dim == 64 ? launch_rows<64>(P, plan, s) : launch_rows<128>(P, plan, s));

@@ -15,15 +15,6 @@ static __device__ int g_bad_page = 0;     // each file's own
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAZY = 16.f;     // the reference of a softmax follows the maximum once that has moved up by 2^16: fp32 sums and bf16 weights lose nothing by it
 
-// More tiles of rows than run at once, without strided keys: the tiles of keys of all of them, one after the other, are cut into as many equal parts as
-// there are blocks.  The order is (sequence, tile of rows, key head); a part that begins or ends within a tile of rows leaves sums.
-struct Even {
-  int64_t* prefix;        // [entries + 1]: tiles of keys, times key heads, ahead of an entry (sequence, tile of rows)
-  int2* entry;            // [most]
-  int32_t* first;         // [batch + 1]: a sequence's first entry; first[batch]: entries
-  int most, blocks, rows; // room for entries, blocks of the launch, rows of a tile
-};
-
 struct Params {
   Cache C;
   Batch B;
@@ -37,7 +28,6 @@ struct Params {
   int splits, least;      // most ranges of a list, and the least units of one (plan)
   float* part_o;          // [splits][tokens * heads][D]: sums against part_m, [splits][tokens * heads][2]: reference and sum of weights
   float* part_m;
-  Even even;              // then part_o: [blocks][2][128][D], part_m the same
 };
 
 constexpr int UNIT = 64;  // keys of a list that stay together
@@ -122,10 +112,8 @@ struct Plan {
   int rows;               // of a tile
   int count;              // tiles of a sequence in the grid
   int splits, least;
-  bool even;
 };
 // the form for many rows (mst_paged_tiles.cu); MST_ERR_SHAPE where the queries cannot be described to the TMA unit
 mst_status_t launch_tiles(const Params& P, const Plan& plan, cudaStream_t s);
-int even_blocks(int D);
 
 }  // namespace mst_paged

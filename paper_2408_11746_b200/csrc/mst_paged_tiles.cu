@@ -159,7 +159,7 @@ __device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[64])
 // mask of every tile (DENSE: short strides).  Code that is only jumped over costs registers here.
 enum Mode { NEAR, FAR, DENSE };
 
-template <int D_, Mode MODE, bool EVEN>
+template <int D_, Mode MODE>
 __global__ void __launch_bounds__(THREADS, Shape<D_>::BLOCKS)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                    const __grid_constant__ TileParams A) {
@@ -204,70 +204,20 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
 
+  const int kvh = (int)blockIdx.x % P.C.kv_heads, split = (int)blockIdx.x / P.C.kv_heads, b = (int)blockIdx.y;
   const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
+  const int len = P.B.len[b], have = (int)(len < reach ? len : reach);       // positions that there are
+  // late tiles have the most keys and come first
+  const int64_t all = P.B.first[b + 1] > P.B.first[b] ? ((int64_t)P.B.first[b + 1] - P.B.first[b]) * P.group : 0;
+  const int tiles = (int)((all + A.rows - 1) / A.rows);
   uint32_t lap = 0, far_lap = 0;   // tiles of rows so far, those with strided keys: barriers that complete once in each
   uint32_t base_t = 0;  // near tiles so far: ring places go on from tile to tile
-  // One tile of rows after another.  EVEN: the block's part of all tiles of keys, at .. end - 1, from entry e on; otherwise a (key head, range,
-  // sequence) and every A.count-th tile of its rows, late ones, which have the most keys, first.
-  int64_t at = 0, end = 0;
-  int e = 0, kvh = 0, split = 0, b = 0, tiles = 0, z = (int)blockIdx.z;
-  if (EVEN) {
-    __shared__ int entry_sh;
-    const int entries = P.even.first[P.B.batch];
-    const int64_t total = P.even.prefix[entries];
-    at = total * (int)blockIdx.x / P.even.blocks;
-    end = total * ((int)blockIdx.x + 1) / P.even.blocks;
-    for (int i = (int)threadIdx.x; i < entries; i += THREADS)
-      if (P.even.prefix[i] <= at && at < P.even.prefix[i + 1]) entry_sh = i;
-    __syncthreads();
-    e = entry_sh;
-  } else {
-    kvh = (int)blockIdx.x % P.C.kv_heads;
-    split = (int)blockIdx.x / P.C.kv_heads;
-    b = (int)blockIdx.y;
-    const int64_t all = P.B.first[b + 1] > P.B.first[b] ? ((int64_t)P.B.first[b + 1] - P.B.first[b]) * P.group : 0;
-    tiles = (int)((all + A.rows - 1) / A.rows);
-  }
-  for (;;) {
-    int tile, off = 0, take = 0;
-    if (EVEN) {
-      if (at >= end) break;
-      const int64_t ahead = P.even.prefix[e], behind = P.even.prefix[e + 1];
-      const int cost = (int)((behind - ahead) / P.C.kv_heads);
-      kvh = (int)((at - ahead) / cost);
-      off = (int)(at - ahead - (int64_t)kvh * cost);
-      take = cost - off < end - at ? cost - off : (int)(end - at);
-      const int2 entry = P.even.entry[e];
-      b = entry.x;
-      tile = entry.y;
-      at += take;
-      if (at == behind) ++e;
-    } else {
-      if (z >= tiles) break;
-      tile = tiles - 1 - z;
-      z += A.count;
-    }
-    const int len = P.B.len[b], have = (int)(len < reach ? len : reach);       // positions that there are
+  for (int z = (int)blockIdx.z; z < tiles; z += A.count) {
     List T;
-    if (!locate(T, P, b, tile, A.rows)) break;
+    if (!locate(T, P, b, tiles - 1 - z, A.rows)) break;
     const TileWalk walk(T, reach);
-    int n0, n1, m0, m1;
-    bool whole;           // this block has all of the tile's keys
-    if (EVEN) {
-      n0 = off < walk.near ? off : walk.near;
-      n1 = off + take < walk.near ? off + take : walk.near;
-      whole = off == 0 && n1 == walk.near;
-      m0 = walk.m_first;
-      m1 = off == 0 ? m0 + walk.far : m0;
-    } else {
-      int active;
-      if (!walk.range(P.splits, P.least, split, n0, n1, m0, m1, active)) continue;
-      whole = active == 1;
-    }
-    // where a row's sums go if not
-    auto part_of = [&](int row, int64_t token, int h) {
-      return EVEN ? ((int64_t)blockIdx.x * 2 + (off == 0 ? 1 : 0)) * ROWS + row : ((int64_t)split * P.B.tokens + token) * P.heads + h;
-    };
+    int n0, n1, m0, m1, active;
+    if (!walk.range(P.splits, P.least, split, n0, n1, m0, m1, active)) continue;
     const int near = n1 - n0, key0 = walk.first + n0 * KEYS;
     if (near == 0) {      // no row has a position
       if (warp < CW)
@@ -651,7 +601,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const float mm = fmaxf(ma, mb);
       float a0 = ex2(ma - mst_paged::reference(mm)), a1 = ex2(mb - mst_paged::reference(mm));
       const float total = fmaf(a0, stat[ROWS + r], a1 * stat[3 * ROWS + r]);
-      if (whole) {
+      if (active == 1) {
         const float inv = total == 0.f ? 0.f : 1.f / total;
         a0 *= inv;
         a1 *= inv;
@@ -660,7 +610,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
       const bool ok = __all_sync(0xffffffffu, *abort_flag == 0);
       tc_fence_after();
       const int t = live ? (T.row0 + r) / P.group : 0, h = kvh * P.group + (live ? (T.row0 + r) % P.group : 0);
-      const int64_t token = T.first + t, part = part_of(r, token, h);
+      const int64_t token = T.first + t, at = ((int64_t)split * P.B.tokens + token) * P.heads + h;
       bool bad = !(total * 0.f == 0.f) || (MODE == NEAR && m1 > m0);     // (a length beyond what the table has room for: see launch)
 #pragma unroll
       for (int pc = 0; pc < HALF / 16; ++pc) {
@@ -678,26 +628,26 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           u[e] = __float_as_uint(o);
         }
         bad = bad || !(check == 0.f);
-        if (whole) {
+        if (active == 1) {
           stage_row(own + (uint32_t)(c / 64) * 2 * TILE_BYTES, r, c % 64, u, 1.f);
         } else if (live && ok) {
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(P.part_o + part * D_ + c + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(P.part_o + at * D_ + c + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
         }
       }
       tc_fence_before();
       if (live && ok && half == 0) {
-        if (whole) {
+        if (active == 1) {
           if (P.lse) P.lse[(int64_t)h * P.B.tokens + token] = (mm + log2f(total)) * LN2;
         } else {
-          P.part_m[part * 2] = mm;
-          P.part_m[part * 2 + 1] = total;
+          P.part_m[at * 2] = mm;
+          P.part_m[at * 2 + 1] = total;
         }
       }
       const uint32_t redo = __ballot_sync(0xffffffffu, bad && live && ok);
       if (lane == 0 && redo) atomicOr(&again[quarter], redo);
       softmax_warps_meet();
-      if (whole && ok) {
+      if (active == 1 && ok) {
 #pragma unroll
         for (int it = 0; it < 16; it += 4) {
           const int rr = rs + it + (lane >> 3);
@@ -719,10 +669,10 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           const int hh = kvh * P.group + (T.row0 + rr) % P.group;
           row_again<D_>(P, b, (int)tk, hh, T.p_lo + (T.row0 + rr) / P.group - T.t_lo, key0, have < to_key ? have : (int)to_key, P.l, MODE == DENSE, m0, m1, o,
                         gm, gs);
-          if (whole) {
+          if (active == 1) {
             finish<D_ / 32>(P, tk, hh, lane, o, gm, gs);
           } else {
-            const int64_t to = part_of(rr, tk, hh);
+            const int64_t to = ((int64_t)split * P.B.tokens + tk) * P.heads + hh;
 #pragma unroll
             for (int e = 0; e < D_ / 32; ++e) P.part_o[to * D_ + lane * (D_ / 32) + e] = o[e];
             if (lane == 0) {
@@ -750,120 +700,6 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS) : "memory");
   }
-}
-
-// ---------------------------------------------------------------------------------------------- even parts
-// inclusive sums over a block of 1024
-__device__ __forceinline__ int64_t sums_of(int64_t v, int64_t* warp_sums, int64_t& all) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += u;
-  }
-  __syncthreads();
-  if (lane == 31) warp_sums[warp] = v;
-  __syncthreads();
-  int64_t before = 0;
-  all = 0;
-  for (int k = 0; k < 32; ++k) {
-    if (k < warp) before += warp_sums[k];
-    all += warp_sums[k];
-  }
-  return v + before;
-}
-// the tiles of keys ahead of every (sequence, tile of rows); one block
-__global__ void __launch_bounds__(1024) paged_even_kernel(const __grid_constant__ Params P) {
-  __shared__ int64_t warp_sums[32];
-  mst_grid_launch_dependents();
-  mst_grid_dependency_wait();
-  const Even& V = P.even;
-  int64_t done = 0, all;
-  for (int b0 = 0; b0 < P.B.batch; b0 += 1024) {
-    const int b = b0 + (int)threadIdx.x;
-    int64_t tiles = 0;
-    if (b < P.B.batch) {
-      const int first = P.B.first[b], end = P.B.first[b + 1];
-      if (first >= 0 && end > first && end <= P.B.tokens) tiles = (((int64_t)end - first) * P.group + V.rows - 1) / V.rows;
-    }
-    const int64_t upto = done + sums_of(tiles, warp_sums, all);
-    if (b < P.B.batch) V.first[b + 1] = (int)(upto < V.most ? upto : V.most);     // rows that overlap may ask for more than there are
-    done += all;
-  }
-  if (threadIdx.x == 0) {
-    V.first[0] = 0;
-    V.prefix[0] = 0;
-  }
-  __syncthreads();
-  const int entries = V.first[P.B.batch];
-  const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  done = 0;
-  for (int e0 = 0; e0 < entries; e0 += 1024) {
-    const int e = e0 + (int)threadIdx.x;
-    int64_t cost = 0;
-    if (e < entries) {
-      int lo = 0, hi = P.B.batch - 1;          // the last sequence whose first entry is not behind e
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (V.first[mid] <= e) lo = mid; else hi = mid - 1;
-      }
-      List T;
-      if (locate(T, P, lo, e - V.first[lo], V.rows)) {
-        const int near = TileWalk(T, reach).near;
-        cost = (int64_t)(near > 0 ? near : 1) * P.C.kv_heads;
-      } else {
-        cost = P.C.kv_heads;
-      }
-      V.entry[e] = make_int2(lo, e - V.first[lo]);
-    }
-    const int64_t upto = done + sums_of(cost, warp_sums, all);
-    if (e < entries) V.prefix[e + 1] = upto;
-    done += all;
-  }
-}
-// the part that place x is in
-__device__ __forceinline__ int part_with(int64_t x, int64_t total, int blocks) {
-  int i = (int)(x * blocks / total);
-  while (i + 1 < blocks && total * (i + 1) / blocks <= x) ++i;
-  while (i > 0 && total * i / blocks > x) --i;
-  return i;
-}
-// a warp a row of a tile that several blocks had keys of: the first block's sums are its second ones, the others' their first
-template <int D_>
-__global__ void __launch_bounds__(128) paged_even_join_kernel(const __grid_constant__ Params P) {
-  constexpr int E = D_ / 32;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  mst_grid_launch_dependents();
-  mst_grid_dependency_wait();
-  const int64_t row = (int64_t)blockIdx.x * 4 + warp, token = row / P.heads;
-  if (token >= P.B.tokens) return;
-  const int h = (int)(row - token * P.heads), b = sequence_of(P.B, (int)token, lane);
-  if (b < 0) return;
-  const Even& V = P.even;
-  const int64_t pair = (token - P.B.first[b]) * P.group + h % P.group;
-  const int tile = (int)(pair / V.rows), r = (int)(pair - (int64_t)tile * V.rows), e = V.first[b] + tile;
-  if (e >= V.first[b + 1]) return;
-  const int64_t total = V.prefix[V.first[P.B.batch]], ahead = V.prefix[e], cost = (V.prefix[e + 1] - ahead) / P.C.kv_heads;
-  const int64_t from = ahead + cost * (h / P.group);
-  const int i0 = part_with(from, total, V.blocks), i1 = part_with(from + cost - 1, total, V.blocks);
-  if (i0 == i1) return;
-  auto place = [&](int i) { return ((int64_t)i * 2 + (i == i0 ? 1 : 0)) * ROWS + r; };
-  auto empty = [&](int i) { return total * i / V.blocks == total * (i + 1) / V.blocks; };    // fewer tiles of keys than blocks
-  float mm = -INFINITY, sum = 0.f, o[E];
-  for (int i = i0 + lane; i <= i1; i += 32)
-    if (!empty(i)) mm = fmaxf(mm, P.part_m[place(i) * 2]);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-#pragma unroll
-  for (int k = 0; k < E; ++k) o[k] = 0.f;
-  for (int i = i0; i <= i1; ++i) {
-    if (empty(i)) continue;
-    const float c = ex2(P.part_m[place(i) * 2] - mst_paged::reference(mm));
-    sum = fmaf(c, P.part_m[place(i) * 2 + 1], sum);
-#pragma unroll
-    for (int k = 0; k < E; ++k) o[k] = fmaf(c, P.part_o[place(i) * D_ + lane * E + k], o[k]);
-  }
-  finish<E>(P, token, h, lane, o, mm, sum);
 }
 
 // ---------------------------------------------------------------------------------------------- maps and launch
@@ -905,26 +741,19 @@ bool cache_maps(const Params& P, TileParams& A, CUtensorMap* tmK, CUtensorMap* t
   return encode(tmK, P.C.K, 4, dims, strides, boxes) && encode(tmV, P.C.V, 4, dims, strides, boxes);
 }
 
-template <int D_, Mode MODE, bool EVEN>
+template <int D_, Mode MODE>
 mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
-  MST_SMEM_LIMIT((paged_tiles_kernel<D_, MODE, EVEN>), Shape<D_>::SMEM);
-  const Params& P = A.P;
-  const dim3 grid = EVEN ? dim3((unsigned)P.even.blocks) : dim3((unsigned)(P.C.kv_heads * P.splits), (unsigned)P.B.batch, (unsigned)A.count);
-  if (EVEN) MST_CUDA_TRY(mst_launch_overlapped(paged_even_kernel, dim3(1), dim3(1024), 0, s, P));
-  MST_CUDA_TRY(mst_launch_overlapped(paged_tiles_kernel<D_, MODE, EVEN>, grid, dim3(THREADS), Shape<D_>::SMEM, s, tmQ, tmK, tmV, A));
-  if (EVEN) {
-    const unsigned blocks = (unsigned)(((int64_t)P.B.tokens * P.heads + 3) / 4);
-    MST_CUDA_TRY(mst_launch_overlapped(paged_even_join_kernel<D_>, dim3(blocks), dim3(128), 0, s, P));
-  }
+  MST_SMEM_LIMIT((paged_tiles_kernel<D_, MODE>), Shape<D_>::SMEM);
+  const dim3 grid((unsigned)(A.P.C.kv_heads * A.P.splits), (unsigned)A.P.B.batch, (unsigned)A.count);
+  MST_CUDA_TRY(mst_launch_overlapped(paged_tiles_kernel<D_, MODE>, grid, dim3(THREADS), Shape<D_>::SMEM, s, tmQ, tmK, tmV, A));
   return MST_OK;
 }
 template <int D_>
-mst_status_t launch(const TileParams& A, bool even, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
+mst_status_t launch(const TileParams& A, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s) {
   const int64_t reach = (int64_t)A.P.B.table_stride * A.P.C.page_size;
-  if (A.P.l < DENSE_BELOW) return even ? launch<D_, DENSE, true>(A, tmQ, tmK, tmV, s) : launch<D_, DENSE, false>(A, tmQ, tmK, tmV, s);
-  if (reach / 2 >= A.P.l) return launch<D_, FAR, false>(A, tmQ, tmK, tmV, s);
+  if (A.P.l < DENSE_BELOW) return launch<D_, DENSE>(A, tmQ, tmK, tmV, s);
   // lengths beyond the table's room may still have rows two strides in, which are formed again key by key
-  return even ? launch<D_, NEAR, true>(A, tmQ, tmK, tmV, s) : launch<D_, NEAR, false>(A, tmQ, tmK, tmV, s);
+  return reach / 2 < A.P.l ? launch<D_, NEAR>(A, tmQ, tmK, tmV, s) : launch<D_, FAR>(A, tmQ, tmK, tmV, s);
 }
 
 }  // namespace
@@ -943,9 +772,8 @@ mst_status_t launch_tiles(const Params& P, const Plan& plan, cudaStream_t s) {
   const int box = box_rows(P.C.page_size);
   A.box = box >= 8 && P.C.num_pages > 0 && cache_maps(P, A, &tmK, &tmV, box) ? box : 0;
   if (A.box == 0) tmK = tmV = tmQ;       // not read, but fetched ahead
-  return P.C.D == 64 ? launch<64>(A, plan.even, tmQ, tmK, tmV, s) : launch<128>(A, plan.even, tmQ, tmK, tmV, s);
+  return P.C.D == 64 ? launch<64>(A, tmQ, tmK, tmV, s) : launch<128>(A, tmQ, tmK, tmV, s);
 }
-int even_blocks(int D) { return (D == 64 ? Shape<64>::BLOCKS : Shape<128>::BLOCKS) * mst_sm_count(); }
 }  // namespace mst_paged
 
 mst_status_t mst_paged_tiles_error_flags(int32_t* flags) {
