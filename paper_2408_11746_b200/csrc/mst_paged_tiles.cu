@@ -11,10 +11,12 @@
 //              written it over the scores.
 // Tensor memory: the halves' scores in columns 0-63 and 64-127, their outputs behind: two blocks an SM at head_dim 64.  Ranges of a list (blockIdx.x)
 // leave sums for the join.
-// Bound: the chain of a half through products, exponentials and barriers, four of which an SM has at a time: 3050 clocks a 128 x 128 tile and block,
-// where the exponential unit (16 a clock) needs 1024 for each of the two blocks and the products 640.  4479 tokens of three sequences over 4000 to 12000
-// positions, 12 heads: 272 us, exponential unit 54 % busy.  (Tiles of 64 keys with two score buffers 305 us, tiles of 128 without independent halves
-// 304, one lane that issues by itself 5 us more.)
+// Bound: the chain of a half through products, exponentials and barriers, four of which an SM has at a time: 2900 clocks for a 128 x 128 tile of each of
+// the two blocks, of which the exponential unit (16 a clock) needs 2048 and the products 640.  4479 tokens of three sequences over 4000 to 12000
+// positions, 12 heads: 256 us.  Taken back: tiles of 64 keys with two score buffers (33 us more), tiles of 128 without independent halves (32), one lane
+// that issues by itself (5); an eighth of the exponentials as polynomials (6 us less, a quarter nothing: not worth a second exponential); blocks that
+// take even shares of all tiles' keys (8 us less here, where 432 tiles of rows meet 296 blocks, but 4 x 1024 tokens 26 -> 102, 32 x 512 of 600 82 -> 230:
+// what a block does at its start and end is then done by few blocks one after another).
 #include <cuda.h>
 
 #include <type_traits>
@@ -534,8 +536,9 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           float sum;
 #pragma unroll 1
           for (int pass = 0;; ++pass) {
-            const float nm = -mst_paged::reference(m);
-            float add[4] = {0.f, 0.f, 0.f, 0.f};
+            const float against = -mst_paged::reference(m);
+            const uint64_t nm = pack2(against, against), scale = pack2(P.scale_log2, P.scale_log2);     // two keys an instruction: 272 us without, 256
+            uint64_t add[2] = {0, 0};
             uint32_t x[2][8];
             tmem_ld8_nowait(t_s, x[0]);
 #pragma unroll
@@ -545,14 +548,12 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
               mask(x[g & 1], g);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const float lo = ex2(fmaf(__uint_as_float(x[g & 1][2 * e]), P.scale_log2, nm));
-                const float hi = ex2(fmaf(__uint_as_float(x[g & 1][2 * e + 1]), P.scale_log2, nm));
-                add[e & 1] += lo;
-                add[2 + (e & 1)] += hi;
-                w[4 * g + e] = pack_bf16(lo, hi);
+                const uint64_t weights = ex2_2(fma2(pack2(x[g & 1][2 * e], x[g & 1][2 * e + 1]), scale, nm));
+                add[e & 1] = add2(add[e & 1], weights);
+                w[4 * g + e] = pack_bf16_2(weights);
               }
             }
-            sum = (add[0] + add[1]) + (add[2] + add[3]);
+            sum = halves_sum(add2(add[0], add[1]));
             if (pass == 1 || !__any_sync(0xffffffffu, sum > MOST || (live && m == -INFINITY))) break;
             float top = -INFINITY;
 #pragma unroll 1
