@@ -165,6 +165,13 @@ def test_forms_of_the_attention(mst, max_new, max_len, stride, splits):
     assert n == (splits * 1000 * 4 * 66 * 4 if splits > 1 else 0)
 
 
+def test_form_of_the_attention_with_very_many_strided_keys(mst):
+    """A table with room for 2^18 strided keys of a row or more: few rows, two ranges of 400 blocks."""
+    for table, splits in (((1 << 20) - 4, 5), (1 << 20, 2)):
+        b = _batch(mst, tokens=1000, max_new=800, max_len=20000, table_stride=table)
+        assert mst.mst_paged_attention_workspace(_cache(mst), b, 4, 64) == splits * 1000 * 4 * 66 * 4
+
+
 def test_calls_without_sequences(mst):
     none = _batch(mst, batch=0, first=None, len=None, page_table=None)
     _append(mst, batch=none)
