@@ -297,7 +297,9 @@ mst_status_t mst_paged_append(const mst_paged_cache_t* cache, const mst_paged_ba
  * head h / (heads / kv_heads).  Q: device bf16, rows of ldq elements; Out: device bf16, rows of ldo elements; lse: device float [heads x tokens]
  * or NULL, log sum_j exp(q . k_j / sqrt(d)).  A query without keys gets Out = 0 and lse = -inf.  What S_i leaves out does not reach
  * a result, be it infinite or NaN.  Scores and sums are fp32, the softmax weights are rounded to bf16 before they multiply the values.
- * Supported: head_dim 64 or 128, up to 2^35 elements each of K and V, any positive stride, ldq and ldo multiples of 8, 16-byte aligned pointers; anything else MST_ERR_SHAPE.  No atomics on results: they repeat bit for bit for the same arguments.
+ * Supported: head_dim 64 or 128, up to 2^35 elements each of K and V, any positive stride, ldq and ldo multiples of 8, 16-byte aligned
+ * pointers; anything else MST_ERR_SHAPE.  Out, lse and the workspace overlap nothing else that the call is given.  No atomics on results:
+ * they repeat bit for bit for the same arguments.
  * workspace: device, 16-byte aligned, at least mst_paged_attention_workspace bytes (MST_ERR_CAPACITY otherwise; NULL where that is 0),
  * contents irrelevant before and after the call. */
 mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, int32_t heads, int32_t stride,

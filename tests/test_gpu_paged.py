@@ -115,6 +115,28 @@ def test_attention(heads, kv, D, page, heads_first, shape, stride):
     Case(*shape, heads, kv, D, page, heads_first=heads_first, spare=3, seed=stride % 97 + D).run(stride, pad=8)
 
 
+@pytest.mark.parametrize("page", [16, 12])
+@pytest.mark.parametrize("stride", [FAR, 64])
+@pytest.mark.parametrize("layout", ["slots of all pages side by side", "keys and values of a page side by side", "padded heads", "heads, then slots, then pages"])
+def test_orders_of_the_cache(layout, stride, page):
+    c = Case(*CHUNK, 4, 2, page=page, seed=3).upload()
+    n = c.dK.shape[0]
+    if layout == "slots of all pages side by side":
+        c.dK, c.dV = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in (c.dK, c.dV))
+    elif layout == "keys and values of a page side by side":
+        both = torch.stack([c.dK, c.dV], dim=1)
+        c.dK, c.dV = both[:, 0], both[:, 1]
+    elif layout == "padded heads":
+        pad = torch.full((2, n, page, 3, 72), float("nan"), dtype=torch.bfloat16, device=dev())
+        pad[:, :, :, :2, :64] = torch.stack([c.dK, c.dV])
+        c.dK, c.dV = pad[0][:, :, :2, :64], pad[1][:, :, :2, :64]
+    else:
+        c.dK, c.dV = (t.permute(2, 1, 0, 3).contiguous().permute(2, 1, 0, 3) for t in (c.dK, c.dV))
+    c.cache = mst.PagedCache(c.dK, c.dV)
+    for form in ("few", "tiles", "ranges"):
+        c.check(stride, *c.said(form).attend(stride))
+
+
 @pytest.mark.parametrize("stride", [1, 2, 3, 17, 31])
 def test_short_strides(stride):
     Case([1, 40, 6], [333, 90, 6], 4, 2).run(stride)
