@@ -413,7 +413,7 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   const int64_t tiles = (rows + p.rows - 1) / p.rows;
   p.count = (int)(tiles < 65535 ? tiles : 65535);
   // Long lists are cut into ranges until there are blocks for the whole GPU, two of which an SM holds.  Tiles: for one wave and no more (432 blocks of up to
-  // 94 tiles: cut into 960 9 us more).  Few rows: for two, as lists are of many lengths (long ragged contexts 41.8 us, for six waves 47.9).
+  // 94 tiles: cut into 960 9 us more, when it took 272).  Few rows: for two, as lists are of many lengths (long ragged contexts 41.8 us, for six waves 47.9).
   // units: tiles of 128 keys and strided keys, which take about as long; or 64 entries
   int64_t units, want = 2 * (int64_t)mst_sm_count();
   if (p.tiles) {

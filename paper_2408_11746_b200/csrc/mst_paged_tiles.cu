@@ -13,9 +13,9 @@
 // leave sums for the join.
 // Bound: the chain of a half through products, exponentials and barriers, four of which an SM has at a time: 2900 clocks for a 128 x 128 tile of each of
 // the two blocks, of which the exponential unit (16 a clock) needs 2048 and the products 640.  4479 tokens of three sequences over 4000 to 12000
-// positions, 12 heads: 256 us.  Taken back: tiles of 64 keys with two score buffers (33 us more), tiles of 128 without independent halves (32), one lane
+// positions, 12 heads: 185 us.  Taken back: tiles of 64 keys with two score buffers (33 us more), tiles of 128 without independent halves (32), one lane
 // that issues by itself (5); an eighth of the exponentials as polynomials (6 us less, a quarter nothing: not worth a second exponential); blocks that
-// take even shares of all tiles' keys (8 us less here, where 432 tiles of rows meet 296 blocks, but 4 x 1024 tokens 26 -> 102, 32 x 512 of 600 82 -> 230:
+// take even shares of all tiles' keys (when tiles came sequence by sequence: 8 us less here, but 4 x 1024 tokens 26 -> 102, 32 x 512 of 600 82 -> 230:
 // what a block does at its start and end is then done by few blocks one after another).
 #include <cuda.h>
 
@@ -46,6 +46,8 @@ struct Shape {
 struct TileParams {
   Params P;
   int rows;             // of a tile: whole tokens
+  Divider by_tokens;    // how many, and one over that
+  float per_token;
   int count;            // tiles of a sequence that the grid has
   int box;              // rows of a TMA box, 0: plain copies only
   int at_slot, at_head, at_page;   // which of the map's coordinates 1 .. 3 they are
@@ -161,6 +163,57 @@ __device__ __forceinline__ void start_sums(uint32_t taddr, const float (&a)[64])
 // mask of every tile (DENSE: short strides).  Code that is only jumped over costs registers here.
 enum Mode { NEAR, FAR, DENSE };
 
+// Which tile of rows comes n-th.  Those with the most keys first, so that no long list starts late: a sequence's from its end, and over all sequences where
+// there are 32 at most and they do not end alike.  A warp's question then, each lane with a sequence: tiles lie on levels of as many positions as a tile
+// has tokens, a sequence's on successive ones, and the level that has the n-th is found by halving.  Where one launch has chunks of long and of short
+// sequences: 4479 tokens of three over 4000 to 12000 positions 256 -> 185 us, 4 x 375 to 1500 over 1500 to 9000 164 -> 130, 16 x 512 to 2048 over 2048 to
+// 4000 316 -> 297, stride 256 266 -> 237; where all end alike the question costs 1 to 3 % (16 x 1024 88.4 -> 90.7 us).
+struct Turn {
+  int b, tile, first, end, len;     // a sequence and its tile, -1: none
+  static __device__ __forceinline__ int count(const TileParams& A, int first, int end) {
+    return first >= 0 && end > first && end <= A.P.B.tokens ? A.by_tokens.over(end - first - 1) + 1 : 0;
+  }
+  __device__ __forceinline__ Turn(const TileParams& A, uint32_t z, int lane) {
+    const Batch& B = A.P.B;
+    const bool few = B.batch <= 32;
+    const int mine = few ? (lane < B.batch ? lane : 0) : (int)blockIdx.y;
+    first = B.first[mine];
+    end = B.first[mine + 1];
+    len = B.len[mine];
+    b = (int)blockIdx.y;
+    int tiles = count(A, first, end);
+    tile = tiles - 1 - (int)z;
+    if (!few) return;
+    if (lane >= B.batch) tiles = 0;
+    constexpr float FAR_OFF = 1 << 29;
+    const float level = ((float)len - (float)(end - first)) * A.per_token;       // about: a sequence may be off by a little
+    const int below = (int)fminf(fmaxf(level, -FAR_OFF), FAR_OFF), top = below + tiles;
+    int hi = __reduce_max_sync(0xffffffffu, tiles > 0 ? top : -(1 << 30));
+    if (hi - __reduce_min_sync(0xffffffffu, tiles > 0 ? top : 1 << 30) > 1) {
+      auto from = [&](int level) {      // tiles on this level or above
+        const int n = top - level + 1;
+        return __reduce_add_sync(0xffffffffu, (uint32_t)(n < 0 ? 0 : n < tiles ? n : tiles));
+      };
+      const uint32_t n = blockIdx.y + z * (uint32_t)B.batch;
+      int lo = __reduce_min_sync(0xffffffffu, tiles > 0 ? below + 1 : 1 << 30);
+      while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (from(mid) > n) lo = mid;
+        else hi = mid - 1;
+      }
+      uint32_t on = __ballot_sync(0xffffffffu, lo > below && lo <= top);
+      for (uint32_t skip = n - from(lo + 1); skip > 0 && on; --skip) on &= on - 1;
+      b = on ? __ffs(on) - 1 : 0;
+      tile = on ? __reduce_max_sync(0xffffffffu, lane == b ? lo - 1 - below : -1) : -1;
+    } else {
+      tile = __shfl_sync(0xffffffffu, tile, b);
+    }
+    first = __shfl_sync(0xffffffffu, first, b);
+    end = __shfl_sync(0xffffffffu, end, b);
+    len = __shfl_sync(0xffffffffu, len, b);
+  }
+};
+
 template <int D_, Mode MODE>
 __global__ void __launch_bounds__(THREADS, Shape<D_>::BLOCKS)
 paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -206,17 +259,16 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
   mst_grid_launch_dependents();
   mst_grid_dependency_wait();
 
-  const int kvh = (int)blockIdx.x % P.C.kv_heads, split = (int)blockIdx.x / P.C.kv_heads, b = (int)blockIdx.y;
+  const int kvh = (int)blockIdx.x % P.C.kv_heads, split = (int)blockIdx.x / P.C.kv_heads;
   const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  const int len = P.B.len[b], have = (int)(len < reach ? len : reach);       // positions that there are
-  // late tiles have the most keys and come first
-  const int64_t all = P.B.first[b + 1] > P.B.first[b] ? ((int64_t)P.B.first[b + 1] - P.B.first[b]) * P.group : 0;
-  const int tiles = (int)((all + A.rows - 1) / A.rows);
   uint32_t lap = 0, far_lap = 0;   // tiles of rows so far, those with strided keys: barriers that complete once in each
   uint32_t base_t = 0;  // near tiles so far: ring places go on from tile to tile
-  for (int z = (int)blockIdx.z; z < tiles; z += A.count) {
+  for (uint32_t z = blockIdx.z;; z += (uint32_t)A.count) {
+    const Turn turn_of(A, z, lane);
+    const int b = turn_of.b, len = turn_of.len, have = (int)(len < reach ? len : reach);       // positions that there are
     List T;
-    if (!locate(T, P, b, tiles - 1 - z, A.rows)) break;
+    if (turn_of.tile < 0 || !T.locate(turn_of.first, turn_of.end, len, P.B.tokens, P.by_group, P.by_l, reach, turn_of.tile, A.rows)) break;
+    if (len > reach) g_bad_page = 1;
     const TileWalk walk(T, reach);
     int n0, n1, m0, m1, active;
     if (!walk.range(P.splits, P.least, split, n0, n1, m0, m1, active)) continue;
@@ -537,7 +589,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
 #pragma unroll 1
           for (int pass = 0;; ++pass) {
             const float against = -mst_paged::reference(m);
-            const uint64_t nm = pack2(against, against), scale = pack2(P.scale_log2, P.scale_log2);     // two keys an instruction: 272 us without, 256
+            const uint64_t nm = pack2(against, against), scale = pack2(P.scale_log2, P.scale_log2);     // two keys an instruction: 6 % less time
             uint64_t add[2] = {0, 0};
             uint32_t x[2][8];
             tmem_ld8_nowait(t_s, x[0]);
@@ -764,6 +816,8 @@ mst_status_t launch_tiles(const Params& P, const Plan& plan, cudaStream_t s) {
   TileParams A = {};
   A.P = P;
   A.rows = plan.rows;
+  A.by_tokens = Divider::of((uint32_t)(plan.rows / P.group));
+  A.per_token = (float)P.group / (float)plan.rows;
   A.count = plan.count;
   CUtensorMap tmQ, tmK = {}, tmV = {};
   const cuuint64_t dims[3] = {(cuuint64_t)P.C.D, (cuuint64_t)P.heads, (cuuint64_t)P.B.tokens};

@@ -137,6 +137,16 @@ def test_orders_of_the_cache(layout, stride, page):
         c.check(stride, *c.said(form).attend(stride))
 
 
+@pytest.mark.parametrize("stride", [FAR, 200])
+@pytest.mark.parametrize("heads,kv", [(2, 2), (5, 1), (40, 1)])
+def test_tiles_of_many_sequences(heads, kv, stride):
+    # long and short sequences that end far apart or alike, none, 32 and more of them
+    Case([300, 1, 0, 520, 129, 260], [900, 1500, 10, 520, 2600, 2500], heads, kv, seed=1, spare=2).run(stride)
+    Case([300, 290, 310], [700, 690, 705], heads, kv, seed=2).run(stride)
+    Case([(7 * i) % 50 for i in range(32)], [60 + (37 * i) % 500 for i in range(32)], heads, kv, seed=3).run(stride)
+    Case([(7 * i) % 50 for i in range(33)], [60 + (37 * i) % 500 for i in range(33)], heads, kv, seed=4).run(stride)
+
+
 @pytest.mark.parametrize("stride", [1, 2, 3, 17, 31])
 def test_short_strides(stride):
     Case([1, 40, 6], [333, 90, 6], 4, 2).run(stride)
