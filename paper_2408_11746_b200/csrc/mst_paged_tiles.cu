@@ -169,7 +169,7 @@ enum Mode { NEAR, FAR, DENSE };
 // sequences: 4479 tokens of three over 4000 to 12000 positions 256 -> 185 us, 4 x 375 to 1500 over 1500 to 9000 164 -> 130, 16 x 512 to 2048 over 2048 to
 // 4000 316 -> 297, stride 256 266 -> 237; where all end alike the question costs 1 to 3 % (16 x 1024 88.4 -> 90.7 us).
 struct Turn {
-  int b, tile, first, end, len;     // a sequence and its tile, -1: none
+  int b, tile, first, end, len;     // a sequence, its tile (-1: none), its rows and its length
   static __device__ __forceinline__ int count(const TileParams& A, int first, int end) {
     return first >= 0 && end > first && end <= A.P.B.tokens ? A.by_tokens.over(end - first - 1) + 1 : 0;
   }
