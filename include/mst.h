@@ -265,14 +265,15 @@ typedef struct {
 /* The sequences of one step.  Sequence b has rows first[b] .. first[b + 1] - 1 of the token-major activations as its new tokens (none
  * is allowed) and holds len[b] tokens with them: the new ones are at its last positions, position p in slot p mod page_size of
  * page page_table[b * table_stride + p / page_size].
- *   first        device int32 [batch + 1], ascending
+ *   first        device int32 [batch + 1], ascending from 0 or more to `tokens` at most
  *   len          device int32 [batch]
  *   page_table   device int32 [batch x table_stride]; entries of pages that a length does not reach are not read
  *   tokens       rows of the activations; rows from first[batch] on belong to no sequence: outputs there are left as they were
  *   max_new, max_len   about the largest count of new tokens and the largest length: they decide how the work is cut up, so they go into
  *                speed and the order of sums; every length is served whatever they say
- * first, len and the table live on the device and are checked there: a token at a negative position (len[b] below its new tokens)
- * attends to nothing, and an append passes it over; a page entry outside [0, num_pages), or a position at or beyond table_stride * page_size, is
+ * first, len and the table live on the device and are checked there: of a sequence whose rows go beyond `tokens` those below it are served, at
+ * their own positions, and one that starts below row 0 is passed over, in either call; both set bit 6 of mst_device_error_flags.  A token at a
+ * negative position (len[b] below its new tokens) attends to nothing, and an append passes it over; a page entry outside [0, num_pages), or a position at or beyond table_stride * page_size, is
  * left out (not written, not attended to) and sets bit 4 of mst_device_error_flags. */
 typedef struct {
   int32_t batch, tokens, max_new, max_len;
@@ -428,7 +429,8 @@ mst_status_t mst_er_densities(int32_t n_layers, const int32_t* out_features, con
  * contraction expired and the block gave up; its output is then undefined; bit 1: the same in the attention
  * kernel; bit 2: the same in the structured-sparse contraction;
  * bit 3: the same in the CUDA-core SpMM / SDDMM; bit 4: a page of a cache that does not exist was named, see mst_paged_batch_t,
- * since the last call of this function, which clears it; bit 5: a bounded wait inside the paged attention expired).  Synchronises the device. */
+ * since the last call of this function, which clears it; bit 5: a bounded wait inside the paged attention expired;
+ * bit 6: a sequence of a step had rows outside 0 .. tokens - 1, since the last call as well).  Synchronises the device. */
 mst_status_t mst_device_error_flags(int32_t* flags);
 
 /* The same step without the final wait: inputs are copied on a copy-in stream owned by the layer, the three products

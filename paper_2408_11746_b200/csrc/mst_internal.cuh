@@ -232,7 +232,8 @@ mst_status_t mst_split_error_flags(int32_t* flags);
 // sticky error word of the attention kernel's bounded waits (mst_attention.cu)
 mst_status_t mst_attention_error_flags(int32_t* flags);
 mst_status_t mst_attention_bwd_error_flags(int32_t* flags);
-// bit 0: pages that do not exist were named (cleared by this call), bit 1: bounded waits (mst_paged_attention.cu); the append's bit 0 (mst_rotate.cu)
+// bit 0: pages that do not exist were named, bit 2: sequences with rows outside the activations (both cleared by this call), bit 1: bounded waits
+// (mst_paged_attention.cu); the append's bits 0 and 2 (mst_rotate.cu)
 mst_status_t mst_paged_error_flags(int32_t* flags);
 mst_status_t mst_paged_tiles_error_flags(int32_t* flags);
 mst_status_t mst_append_error_flags(int32_t* flags);

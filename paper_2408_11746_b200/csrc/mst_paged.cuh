@@ -57,21 +57,26 @@ __device__ __forceinline__ Slot slot_of(const Cache& C, const Batch& B, int b, i
   }
   return Slot{true, (int64_t)id * C.page_stride + (int64_t)slot * C.token_stride};
 }
-// The sequence that a row belongs to (a warp's question, all lanes the same row): how many sequences end at or before it.  -1: none
-__device__ __forceinline__ int sequence_of(const Batch& B, int row, int lane) {
+// The sequence that a row belongs to (a warp's question, all lanes the same row): how many sequences end at or before it.  -1: none, or one that
+// RowsOf gives no rows.  `flag`: the file's own word for sequences with rows outside 0 .. tokens - 1
+__device__ __forceinline__ int sequence_of(const Batch& B, int row, int lane, int* flag) {
   int before = 0;
   for (int i0 = 0; i0 < B.batch; i0 += 32) {
-    const bool ended = i0 + lane < B.batch && B.first[i0 + lane + 1] <= row;
-    before += __popc(__ballot_sync(0xffffffffu, ended));
+    const int end = i0 + lane < B.batch ? B.first[i0 + lane + 1] : INT32_MIN;
+    if (end > B.tokens) *flag = 1;
+    before += __popc(__ballot_sync(0xffffffffu, i0 + lane < B.batch && end <= row));
   }
-  return before < B.batch && B.first[before] <= row && row < B.first[before + 1] ? before : -1;
+  if (before >= B.batch) return -1;
+  const int first = B.first[before];
+  if (first < 0) *flag = 1;
+  return first >= 0 && first <= row && row < B.first[before + 1] ? before : -1;
 }
 // The position of row `row` of sequence b, below 0 where the sequence is shorter than its new tokens
 __device__ __forceinline__ int position_of(const Batch& B, int b, int row) {
   const int64_t p = (int64_t)B.len[b] - B.first[b + 1] + row;
   return p < 0 ? -1 : (int)p;
 }
-// A file's word for pages that do not exist: its value, and zero from then on
+// A file's word for pages that do not exist, or for rows: its value, and zero from then on
 inline mst_status_t take_flag(const void* symbol, int32_t* flag) {
   int v = 0;
   MST_CUDA_TRY(cudaMemcpyFromSymbol(&v, symbol, sizeof(int)));

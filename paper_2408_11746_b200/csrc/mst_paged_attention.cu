@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
   mst_grid_dependency_wait();
   const int64_t row = (int64_t)blockIdx.x * 4 + warp, token = row / P.heads;
   if (token >= P.B.tokens) return;
-  const int h = (int)(row - token * P.heads), b = sequence_of(P.B, (int)token, lane);
+  const int h = (int)(row - token * P.heads), b = sequence_of(P.B, (int)token, lane, &g_bad_rows);
   if (b < 0) return;
   const int64_t pair = (token - P.B.first[b]) * P.group + h % P.group;
   List T;
@@ -474,10 +474,11 @@ mst_status_t check_attention(const mst_paged_cache_t* cache, const mst_paged_bat
 }  // namespace
 
 mst_status_t mst_paged_error_flags(int32_t* flags) {
-  int32_t rows = 0, tiles = 0;
-  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_page, &rows));
+  int32_t pages = 0, rows = 0, tiles = 0;
+  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_page, &pages));
+  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_rows, &rows));
   MST_TRY(mst_paged_tiles_error_flags(&tiles));
-  *flags = rows | tiles;
+  *flags = pages | (rows << 2) | tiles;
   return MST_OK;
 }
 

@@ -10,7 +10,7 @@ namespace mst_paged {
 using namespace mst_ptx;
 using mst_att::ex2;
 
-static __device__ int g_bad_page = 0;     // each file's own
+static __device__ int g_bad_page = 0, g_bad_rows = 0;     // each file's own
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LAZY = 16.f;     // the reference of a softmax follows the maximum once that has moved up by 2^16: fp32 sums and bf16 weights lose nothing by it
@@ -34,10 +34,11 @@ constexpr int UNIT = 64;  // keys of a list that stay together
 
 // A tile of sequence b (mst_paged_list.h)
 __device__ __forceinline__ bool locate(List& T, const Params& P, int b, int tile, int R) {
-  const int len = P.B.len[b];
+  const RowsOf rows(P.B.first[b], P.B.first[b + 1], P.B.len[b], P.B.tokens);
   const int64_t reach = (int64_t)P.B.table_stride * P.C.page_size;
-  if (!T.locate(P.B.first[b], P.B.first[b + 1], len, P.B.tokens, P.by_group, P.by_l, reach, tile, R)) return false;
-  if (len > reach) g_bad_page = 1;
+  if (rows.outside) g_bad_rows = 1;
+  if (!T.locate(rows.first, rows.end, rows.len, P.B.tokens, P.by_group, P.by_l, reach, tile, R)) return false;
+  if (rows.len > reach) g_bad_page = 1;
   return true;
 }
 

@@ -36,6 +36,18 @@ struct Divider {
   }
 };
 
+// The rows first .. end - 1 of a sequence that the activations' `tokens` rows have: those beyond them are cut off, positions counted from the true end
+// (so a length goes down with it; below 0 nobody has a position either way).  One that starts below 0 has none, which `locate` sees to.
+struct RowsOf {
+  int first, end, len;
+  bool outside;       // some rows, or the place of none, are not among the activations'
+  MST_HD RowsOf(int first_, int end_, int len_, int tokens) : first(first_) {
+    end = end_ < tokens ? end_ : tokens;
+    len = len_ < 0 ? len_ : len_ - (end_ - end);
+    outside = first < 0 || end_ > tokens;
+  }
+};
+
 struct Key {
   int pos;    // -1: none
   int who;    // the token of the tile that alone looks at it, -1: the window

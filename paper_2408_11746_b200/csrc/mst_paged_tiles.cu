@@ -169,17 +169,19 @@ enum Mode { NEAR, FAR, DENSE };
 // sequences: 4479 tokens of three over 4000 to 12000 positions 256 -> 185 us, 4 x 375 to 1500 over 1500 to 9000 164 -> 130, 16 x 512 to 2048 over 2048 to
 // 4000 316 -> 297, stride 256 266 -> 237; where all end alike the question costs 1 to 3 % (16 x 1024 88.4 -> 90.7 us).
 struct Turn {
-  int b, tile, first, end, len;     // a sequence, its tile (-1: none), its rows and its length
-  static __device__ __forceinline__ int count(const TileParams& A, int first, int end) {
-    return first >= 0 && end > first && end <= A.P.B.tokens ? A.by_tokens.over(end - first - 1) + 1 : 0;
+  int b, tile, first, end, len;     // a sequence, its tile (-1: none), its rows and its length (RowsOf)
+  static __device__ __forceinline__ int count(const TileParams& A, int first, int end) {      // of RowsOf
+    return first >= 0 && end > first ? A.by_tokens.over(end - first - 1) + 1 : 0;
   }
   __device__ __forceinline__ Turn(const TileParams& A, uint32_t z, int lane) {
     const Batch& B = A.P.B;
     const bool few = B.batch <= 32;
     const int mine = few ? (lane < B.batch ? lane : 0) : (int)blockIdx.y;
-    first = B.first[mine];
-    end = B.first[mine + 1];
-    len = B.len[mine];
+    const RowsOf rows(B.first[mine], B.first[mine + 1], B.len[mine], B.tokens);
+    if (rows.outside) g_bad_rows = 1;
+    first = rows.first;
+    end = rows.end;
+    len = rows.len;
     b = (int)blockIdx.y;
     int tiles = count(A, first, end);
     tile = tiles - 1 - (int)z;
@@ -832,10 +834,11 @@ mst_status_t launch_tiles(const Params& P, const Plan& plan, cudaStream_t s) {
 }  // namespace mst_paged
 
 mst_status_t mst_paged_tiles_error_flags(int32_t* flags) {
-  int32_t bad = 0;
+  int32_t bad = 0, rows = 0;
   int v = 0;
   MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_page, &bad));
+  MST_TRY(mst_paged::take_flag((const void*)&mst_paged::g_bad_rows, &rows));
   MST_CUDA_TRY(cudaMemcpyFromSymbol(&v, g_wait_error, sizeof(int)));
-  *flags = bad | (v << 1);
+  *flags = bad | (v << 1) | (rows << 2);
   return MST_OK;
 }

@@ -9,7 +9,7 @@
 namespace {
 using namespace mst_rot;
 
-__device__ int g_bad_page = 0;
+__device__ int g_bad_page = 0, g_bad_rows = 0;
 
 struct RowsParams {
   Rotation R;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
   int pos;
   mst_paged::Slot slot = {true, 0};
   if (APPEND) {
-    const int b = mst_paged::sequence_of(P.batch, token, lane);
+    const int b = mst_paged::sequence_of(P.batch, token, lane, &g_bad_rows);
     if (b < 0) return;
     pos = mst_paged::position_of(P.batch, b, token);
     if (pos < 0) return;
@@ -371,7 +371,13 @@ mst_status_t check_ld(int64_t ld, int32_t hq, int32_t hk, int D) {
 
 }  // namespace
 
-mst_status_t mst_append_error_flags(int32_t* flags) { return mst_paged::take_flag((const void*)&g_bad_page, flags); }
+mst_status_t mst_append_error_flags(int32_t* flags) {
+  int32_t pages = 0, rows = 0;
+  MST_TRY(mst_paged::take_flag((const void*)&g_bad_page, &pages));
+  MST_TRY(mst_paged::take_flag((const void*)&g_bad_rows, &rows));
+  *flags = pages | (rows << 2);
+  return MST_OK;
+}
 
 extern "C" mst_status_t mst_qk_norm_rotate_fwd(const mst_rotation_t* rotation, mst_dtype_t dtype, int64_t tokens, int32_t seq_len,
                                                const int32_t* positions, int32_t heads_q, int32_t heads_k, const void* Q,

@@ -61,6 +61,13 @@ int near(int first, int end, int len, int tokens, int group, int stride, int64_t
   return mst_paged::near_sees(T.l, p, k);
 }
 
+// first, end, len; 1 where rows were left out
+int rows_of(int first, int end, int len, int tokens, int32_t* out) {
+  const mst_paged::RowsOf r(first, end, len, tokens);
+  out[0] = r.first; out[1] = r.end; out[2] = r.len;
+  return r.outside;
+}
+
 int over(uint32_t d, int n) { return Divider::of(d).over(n); }
 
 int page(const int32_t* row, int table_stride, int page_size, int num_pages, int p, int* slot) {

@@ -19,6 +19,7 @@ if torch.cuda.is_available():
 EPS = 1e-5
 FAR = 1 << 30
 BAD_PAGE = 16
+ROWS_OUTSIDE = 64
 
 
 class Case:
@@ -265,6 +266,29 @@ def test_lengths_and_rows_that_make_no_sense():
             mst.mst_device_error_flags()
 
 
+def _cut(c, tokens):
+    """What the oracle is told of a step whose rows go beyond `tokens`: those below it, where they are."""
+    beyond = np.maximum(c.first[1:].astype(np.int64) - np.maximum(c.first[:-1], tokens), 0)
+    c.length = (np.array(c.length) - beyond).tolist()
+    c.first = np.minimum(c.first, tokens)
+    c.rows = tokens
+
+
+@pytest.mark.parametrize("ahead", [0, 32])
+@pytest.mark.parametrize("stride", [FAR, 64, 7])
+def test_rows_beyond_the_activations(stride, ahead):
+    # one sequence is cut short by the number of rows, one lies behind it: what rows there are is served, and the call says so
+    c = Case([1] * ahead + [3, 40, 60, 5], [9] * ahead + [50, 300, 400, 70], 4, 2)
+    c.tokens = 70 + ahead
+    c.Q = c.Q[: c.tokens].contiguous()
+    c.upload()
+    _cut(c, c.tokens)
+    for form in ("true", "few", "tiles", "ranges", "far", "again"):
+        out, z = c.said(form).attend(stride)
+        c.check(stride, out, z, flags=ROWS_OUTSIDE)
+    assert mst.mst_device_error_flags() == 0
+
+
 def test_no_lse_and_repeats():
     for new, length, form in (([1, 1], [5000, 300], "true"), ([100, 300], [2000, 300], "true"), ([100, 300], [2000, 300], "tiles"), ([100, 300], [6000, 300], "far")):
         c = Case(new, length, 4, 2).upload().said(form)
@@ -418,6 +442,44 @@ def test_append_without_rotation_or_queries_and_with_bad_pages():
     _, K, V, _ = _append_ref(c, x.double().numpy(), np.zeros(0), [None, None], 0, False)
     np.testing.assert_array_equal(host(c.dK), K)
     np.testing.assert_array_equal(host(c.dV), V)
+
+
+@pytest.mark.parametrize("first", [[0, 3, 43, 103], [0, 3, 43, 70, 103], [-2, 3, 43]])
+@pytest.mark.parametrize("form", ["few", "tiles"])
+def test_append_and_attention_of_rows_that_are_not_there(first, form):
+    # a step with rows beyond the activations (70 of them), or below: both calls serve the same rows, and both say so
+    new = np.diff(first).tolist()
+    c = Case(new, [n + 200 for n in new], 4, 2)
+    c.tokens = min(70, first[-1])
+    c.Q = c.Q[: c.tokens].contiguous()
+    c.first = np.array(first, np.int32)
+    c.upload().said(form)
+    r, f, gamma = _rotation(64, 64, False, True)
+    x = torch.randn(c.tokens, 8, 64).to(torch.bfloat16)
+    d = x.view(c.tokens, -1).to(dev())
+    q = torch.full((c.tokens, 256), 7.0, dtype=torch.bfloat16, device=dev())
+    at = lambda h: d.data_ptr() + 128 * h
+    mst.mst_paged_append(c.cache, c.batch, r, 4, at(0), at(4), at(6), 512, q, 256)
+    torch.cuda.synchronize()
+    assert mst.mst_device_error_flags() == ROWS_OUTSIDE and mst.mst_device_error_flags() == 0
+    _cut(c, c.tokens)
+    lo = 0
+    if c.first[0] < 0:           # the oracle has no such rows: the sequence goes, its row of the table too
+        lo = int(c.first[1])
+        c.first, c.length, c.table = c.first[1:] - lo, c.length[1:], c.table[1:]
+        c.rows -= lo
+    ref_q, K, V, _ = _append_ref(c, x.double().numpy()[lo:], f, gamma, 64, False)
+    got = host(q)
+    assert (got[:lo] == 7.0).all()
+    here = got[lo:].reshape(c.rows, 4, 64)
+    assert (np.abs(here - ref_q) <= 2.0 ** -8 * np.abs(ref_q) + 2e-6 * rotation.pair_sizes(ref_q, 64, False) + 1e-30).all()
+    np.testing.assert_array_equal(host(c.dV), V)
+    assert (np.abs(host(c.dK) - K) <= 2.0 ** -8 * np.abs(K) + 2e-6 * rotation.pair_sizes(K, 64, False) + 1e-30).all()
+    c.Q, c.K, c.V = q.cpu(), c.dK.cpu(), c.dV.cpu()
+    out, z = c.attend(128)
+    assert (out[:lo] == 7.0).all() and (z[:, :lo] == 7.0).all()
+    c.Q, c.tokens = c.Q[lo:], c.tokens - lo
+    c.check(128, out[lo:], z[:, lo:], flags=ROWS_OUTSIDE)
 
 
 def test_append_in_place_queries():

@@ -185,3 +185,21 @@ def test_quotients_without_division(lib):
         ns = {0, 1, d - 1, d, min(d + 1, top), top, top - 1, top // d * d, max(top // d * d - 1, 0)} | set(rng.integers(0, top, 200).tolist())
         for n in ns:
             assert lib.over(ctypes.c_uint32(d), ctypes.c_int(n)) == n // d
+
+
+@pytest.mark.parametrize("first,end,length,tokens,want", [
+    (4, 10, 100, 10, (10, 100, 0)), (4, 11, 100, 10, (10, 99, 1)), (0, 50, 50, 10, (10, 10, 1)), (4, 14, 6, 10, (10, 2, 1)),
+    (10, 11, 100, 10, (10, 99, 1)), (1 << 30, (1 << 31) - 1, 5, 0, (0, 5 - (1 << 31) + 1, 1)), (-1, 3, 100, 10, (3, 100, 1)),
+    (5, 4, 100, 10, (4, 100, 0)), (10, 10, 0, 10, (10, 0, 0)), (9, (1 << 31) - 1, -(1 << 31), 10, (10, -(1 << 31), 1)),
+    (-(1 << 31), (1 << 31) - 1, (1 << 31) - 1, 0, (0, 0, 1)), (0, -(1 << 31), -5, 10, (-(1 << 31), -5, 0))])
+def test_rows_that_the_activations_do_not_have(lib, first, end, length, tokens, want):
+    """Rows beyond `tokens` are cut off and those before them stay at their positions."""
+    out = (ctypes.c_int32 * 3)()
+    outside = lib.rows_of(first, end, length, tokens, out)
+    assert (*out[1:], outside) == want and out[0] == first
+    info = (ctypes.c_int64 * 9)()
+    there = lib.list_of(out[0], out[1], out[2], tokens, 1, 64, ctypes.c_int64(BIG), 0, 16, info)
+    assert bool(there) == (0 <= first < min(end, tokens))
+    if there and length >= 0:
+        row0, rows, t_lo, nt, p_lo, p_hi = list(info)[:6]
+        assert p_lo == length - (end - first) and p_hi == p_lo + rows - 1
