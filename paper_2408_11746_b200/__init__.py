@@ -60,6 +60,9 @@ class Rotation(ctypes.Structure):
 
     def __init__(self, head_dim: int, rot_dim: int, inv_freq=None, gamma_q=None, gamma_k=None, eps: float = 1e-6,
                  interleaved: bool = False):
+        for t, n in ((inv_freq if rot_dim > 0 else None, rot_dim // 2), (gamma_q, head_dim), (gamma_k, head_dim)):
+            if hasattr(t, "data_ptr") and (t.dim() != 1 or t.shape[0] != n or str(t.dtype) != "torch.float32" or not t.is_contiguous()):
+                raise ValueError("inv_freq [rot_dim / 2], gamma_q and gamma_k [head_dim] are contiguous float32 tensors")
         super().__init__(head_dim, rot_dim, int(bool(interleaved)), eps, _ptr(inv_freq) or None, _ptr(gamma_q), _ptr(gamma_k))
         self.tensors = (inv_freq, gamma_q, gamma_k)
 

@@ -191,3 +191,17 @@ def test_structures_check_their_tensors(mst):
         with pytest.raises(ValueError):
             mst.PagedBatch(*a, 4, 1, 1)
     assert ctypes.sizeof(mst.PagedCache) == 56 and ctypes.sizeof(mst.PagedBatch) == 48 and ctypes.sizeof(mst.Rotation) == 40
+
+
+def test_rotation_checks_its_tensors(mst):
+    """The library reads rot_dim / 2 and head_dim floats at the addresses it is given: tensors that hold something else are refused."""
+    w, f = torch.ones(64), torch.ones(32)
+    for args in ((w, w, w), (f[:31], w, w), (f.double(), w, w), (f.view(2, 16), w, w), (w[::2], w, w), (f, w.bfloat16(), w), (f, w, w.half()),
+                 (f, w[:63], w), (f, w, torch.ones(128)), (f, torch.ones(128)[::2], w), (f, w, torch.ones(2, 64)), (f.int(), None, None)):
+        with pytest.raises(ValueError):
+            mst.Rotation(64, 64, *args)
+    for args in ((f, w, w), (f, None, w), (f, None, None), (A, A, A), (torch.ones(65)[1:33], torch.ones(128)[64:], w)):
+        mst.Rotation(64, 64, *args)
+    mst.Rotation(64, 0, None, w, w)
+    mst.Rotation(64, 0, torch.empty(0), w, w)
+    mst.Rotation(64, 0, f, None, None)
