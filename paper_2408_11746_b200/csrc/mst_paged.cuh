@@ -29,6 +29,13 @@ inline mst_status_t check(const mst_paged_cache_t* c, const mst_paged_batch_t* b
   if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->page_stride % 8 != 0 || c->token_stride % 8 != 0 ||
       c->head_stride % 8 != 0)
     return MST_ERR_SHAPE;
+  // a cache lies within an address space of 57 bits: products of strides and counts stay in 64
+  int64_t span = c->head_dim;
+  const int64_t dims[3][2] = {{c->head_stride, c->kv_heads}, {c->token_stride, c->page_size}, {c->page_stride, c->num_pages}};
+  for (const int64_t(&x)[2] : dims) {
+    if (x[1] > 1 && x[0] > ((INT64_C(1) << 56) - span) / (x[1] - 1)) return MST_ERR_SHAPE;
+    if (x[1] > 1) span += x[0] * (x[1] - 1);
+  }
   // rows of different slots or heads do not overlap
   if ((c->page_size > 1 && c->token_stride < c->head_dim) || (c->kv_heads > 1 && c->head_stride < c->head_dim) ||
       (c->num_pages > 1 && c->page_stride < c->head_dim))

@@ -205,3 +205,16 @@ def test_rotation_checks_its_tensors(mst):
     mst.Rotation(64, 0, None, w, w)
     mst.Rotation(64, 0, torch.empty(0), w, w)
     mst.Rotation(64, 0, f, None, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(num_pages=1 << 10, page_stride=1 << 58), dict(num_pages=(1 << 10) + 1, page_stride=1 << 57), dict(num_pages=(1 << 31) - 1, page_stride=(1 << 63) - 8),
+    dict(num_pages=2, page_stride=1 << 56), dict(page_size=1 << 30, token_stride=1 << 34, page_stride=1 << 40), dict(page_size=1 << 12, token_stride=1 << 55),
+    dict(kv_heads=1 << 10, head_stride=1 << 58), dict(kv_heads=2, head_stride=1 << 56)])
+def test_strides_beyond_any_address(mst, kw):
+    """Products of strides and counts that do not fit 64 bits are not taken for small ones."""
+    c = _cache(mst, **kw)
+    heads = c.kv_heads
+    assert _status(mst, _append, mst, cache=c, heads=heads, ld=heads * 64, ldq=heads * 64) == SHAPE
+    assert _status(mst, _attend, mst, cache=c, heads=heads, ldq=heads * 64, ldo=heads * 64) == SHAPE
+    assert _status(mst, mst.mst_paged_attention_workspace, c, _batch(mst), heads, 64) == SHAPE
