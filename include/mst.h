@@ -254,7 +254,8 @@ mst_status_t mst_qk_norm_rotate_bwd_workspace(const mst_rotation_t* rotation, in
 
 /* A cache of keys and values in pages of page_size tokens, bf16.  Value d of key head h of the token in slot s of page p is at
  * K[p * page_stride + s * token_stride + h * head_stride + d], V the same: strides in elements, multiples of 8, pointers 16-byte
- * aligned. */
+ * aligned.  Rows do not overlap: in ascending order the stride of each dimension of more than one is at least what those before it span,
+ * the smallest at least head_dim (MST_ERR_SHAPE otherwise). */
 typedef struct {
   void* K;
   void* V;

@@ -3,6 +3,8 @@
 #pragma once
 #include <cuda_bf16.h>
 
+#include <utility>
+
 #include "mst_internal.cuh"
 #include "mst_paged_list.h"
 
@@ -29,17 +31,18 @@ inline mst_status_t check(const mst_paged_cache_t* c, const mst_paged_batch_t* b
   if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 || c->page_stride % 8 != 0 || c->token_stride % 8 != 0 ||
       c->head_stride % 8 != 0)
     return MST_ERR_SHAPE;
-  // a cache lies within an address space of 57 bits: products of strides and counts stay in 64
+  // Rows of different slots or heads do not overlap: with strides in ascending order each is at least what those before it span.  And a cache
+  // lies within an address space of 57 bits: products of strides and counts stay in 64
+  struct { int64_t stride, n; } dims[3] = {{c->head_stride, c->kv_heads}, {c->token_stride, c->page_size}, {c->page_stride, c->num_pages}};
+  for (int i = 0; i < 2; ++i)
+    for (int k = 0; k < 2; ++k)
+      if (dims[k + 1].stride < dims[k].stride) std::swap(dims[k], dims[k + 1]);
   int64_t span = c->head_dim;
-  const int64_t dims[3][2] = {{c->head_stride, c->kv_heads}, {c->token_stride, c->page_size}, {c->page_stride, c->num_pages}};
-  for (const int64_t(&x)[2] : dims) {
-    if (x[1] > 1 && x[0] > ((INT64_C(1) << 56) - span) / (x[1] - 1)) return MST_ERR_SHAPE;
-    if (x[1] > 1) span += x[0] * (x[1] - 1);
+  for (const auto& x : dims) {
+    if (x.n <= 1) continue;
+    if (x.stride < span || x.stride > ((INT64_C(1) << 56) - span) / (x.n - 1)) return MST_ERR_SHAPE;
+    span += x.stride * (x.n - 1);
   }
-  // rows of different slots or heads do not overlap
-  if ((c->page_size > 1 && c->token_stride < c->head_dim) || (c->kv_heads > 1 && c->head_stride < c->head_dim) ||
-      (c->num_pages > 1 && c->page_stride < c->head_dim))
-    return MST_ERR_SHAPE;
   if (((reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V)) & 15u) != 0 ||
       ((reinterpret_cast<uintptr_t>(b->first) | reinterpret_cast<uintptr_t>(b->len) | reinterpret_cast<uintptr_t>(b->page_table)) & 3u) != 0)
     return MST_ERR_SHAPE;

@@ -218,3 +218,27 @@ def test_strides_beyond_any_address(mst, kw):
     assert _status(mst, _append, mst, cache=c, heads=heads, ld=heads * 64, ldq=heads * 64) == SHAPE
     assert _status(mst, _attend, mst, cache=c, heads=heads, ldq=heads * 64, ldo=heads * 64) == SHAPE
     assert _status(mst, mst.mst_paged_attention_workspace, c, _batch(mst), heads, 64) == SHAPE
+
+
+@pytest.mark.parametrize("kw", [
+    dict(token_stride=64, head_stride=64), dict(token_stride=64), dict(token_stride=120), dict(page_stride=64), dict(page_stride=2040),
+    dict(token_stride=64, head_stride=16 * 64 - 8), dict(token_stride=64, head_stride=1024, page_stride=2040),
+    dict(page_stride=64, token_stride=3 * 64 - 8, head_stride=16 * 192), dict(head_stride=56), dict(kv_heads=1, token_stride=56),
+    dict(kv_heads=1, num_pages=1, token_stride=0), dict(page_size=1, kv_heads=1, page_stride=0)])
+def test_caches_whose_rows_overlap(mst, kw):
+    """An append to rows that overlap has no defined result."""
+    c = _cache(mst, **kw)
+    assert _status(mst, _append, mst, cache=c, heads=c.kv_heads) == SHAPE
+    assert _status(mst, _attend, mst, cache=c, heads=c.kv_heads) == SHAPE
+    assert _status(mst, mst.mst_paged_attention_workspace, c, _batch(mst), c.kv_heads, 64) == SHAPE
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(token_stride=64, head_stride=1024), dict(token_stride=136, head_stride=72, page_stride=4096), dict(page_stride=128, token_stride=384),
+    dict(page_stride=16 * 64, token_stride=64, head_stride=3 * 16 * 64), dict(kv_heads=1, head_stride=0, token_stride=64), dict(num_pages=1, page_stride=0),
+    dict(num_pages=0, page_stride=0), dict(page_size=1, token_stride=0, page_stride=128), dict(page_stride=4096)])
+def test_orders_that_are_no_overlap(mst, kw):
+    c = _cache(mst, **kw)
+    none = _batch(mst, tokens=0)
+    _append(mst, cache=c, batch=none, heads=c.kv_heads)
+    _attend(mst, cache=c, batch=none, heads=c.kv_heads)
