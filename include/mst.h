@@ -287,7 +287,8 @@ typedef struct {
 /* The new tokens' keys, normed and rotated by their positions (mst_rotation_t; NULL: as they are), and values into the cache, and the
  * queries, normed and rotated, into Q_out, in one launch.  Q, K, V: device bf16, rows of `ld` elements (slices of a fused activation);
  * Q and Q_out (rows of ldq elements) may be NULL, heads_q is then ignored, or the same with ldq == ld.  Of two tokens that
- * name one slot it is not said whose values, or which of whose, stay. */
+ * name one slot it is not said whose values, or which of whose, stay.  The cache's K and V are different memory (MST_ERR_INVALID_ARG where they
+ * are the same pointer). */
 mst_status_t mst_paged_append(const mst_paged_cache_t* cache, const mst_paged_batch_t* batch, const mst_rotation_t* rotation,
                               int32_t heads_q, const void* Q, const void* K, const void* V, int64_t ld, void* Q_out, int64_t ldq,
                               mst_stream_t stream);

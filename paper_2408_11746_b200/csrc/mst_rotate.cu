@@ -475,6 +475,7 @@ extern "C" mst_status_t mst_paged_append(const mst_paged_cache_t* cache, const m
   if (heads_q > 0) MST_TRY(check_ld(ldq, heads_q, 0, P.R.D));
   if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(Q_out)) return MST_ERR_SHAPE;
   if (P.batch.batch == 0 || P.batch.tokens == 0) return MST_OK;
+  if (cache->K == cache->V) return MST_ERR_INVALID_ARG;      // a row's key and value would be written to one place
   MST_TRY(mst_on_this_device({Q, K, V, Q_out, P.R.inv_freq, P.R.gamma_q, P.R.gamma_k, P.cache.K, P.cache.V, P.batch.first, P.batch.len,
                               P.batch.table}));
   P.Q = Q; P.K = K; P.V = V; P.Qo = Q_out;

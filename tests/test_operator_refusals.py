@@ -242,3 +242,8 @@ def test_orders_that_are_no_overlap(mst, kw):
     none = _batch(mst, tokens=0)
     _append(mst, cache=c, batch=none, heads=c.kv_heads)
     _attend(mst, cache=c, batch=none, heads=c.kv_heads)
+
+
+def test_append_of_keys_and_values_to_one_place(mst):
+    assert _status(mst, _append, mst, cache=_cache(mst, K=A, V=A)) == INVALID
+    _append(mst, cache=_cache(mst, K=A, V=A), batch=_batch(mst, tokens=0))
