@@ -230,6 +230,7 @@ typedef struct {
  * then ignored).  positions: device int32 [tokens], or NULL: token t is at position t mod seq_len.  dtype of Q, K and the results: MST_F32
  * or MST_BF16.  Pointers 16-byte aligned, ld and ldo multiples of 8, otherwise MST_ERR_SHAPE.  In place (Q_out == Q, K_out == K, ldo ==
  * ld) is allowed; other overlaps are not.
+ * With no tokens no row is read or written, and pointers of rows may be NULL, here and in the next calls.
  * This call and the next four take pointers of the current device only: any other (of the host, of another device) is
  * MST_ERR_INVALID_ARG, before anything is launched.  They keep nothing between calls and have no scratch of their own, so calls on
  * different streams, captured ones too, may overlap as long as their outputs and workspaces are different ones. */

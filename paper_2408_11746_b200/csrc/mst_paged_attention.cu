@@ -499,7 +499,7 @@ extern "C" mst_status_t mst_paged_attention(const mst_paged_cache_t* cache, cons
                                             size_t workspace_bytes, mst_stream_t stream) {
   Params P = {};
   MST_TRY(check_attention(cache, batch, heads, stride, &P.C, &P.B));
-  if (!Q || !Out) return MST_ERR_INVALID_ARG;
+  if (batch->tokens > 0 && (!Q || !Out)) return MST_ERR_INVALID_ARG;
   const int64_t width = (int64_t)heads * cache->head_dim;
   if (ldq < width || ldo < width || ldq % 8 != 0 || ldo % 8 != 0) return MST_ERR_SHAPE;
   if (((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(Out) | reinterpret_cast<uintptr_t>(workspace)) & 15u) != 0 ||

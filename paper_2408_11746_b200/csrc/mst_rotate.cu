@@ -388,7 +388,7 @@ extern "C" mst_status_t mst_qk_norm_rotate_fwd(const mst_rotation_t* rotation, m
   MST_TRY(check_rows(dtype, tokens, seq_len, positions, heads_q, heads_k));
   if (heads_q == 0) Q = Q_out = nullptr;
   if (heads_k == 0) K = K_out = nullptr;
-  if ((heads_q > 0 && (!Q || !Q_out)) || (heads_k > 0 && (!K || !K_out))) return MST_ERR_INVALID_ARG;
+  if (tokens > 0 && ((heads_q > 0 && (!Q || !Q_out)) || (heads_k > 0 && (!K || !K_out)))) return MST_ERR_INVALID_ARG;
   MST_TRY(check_ld(ld, heads_q, heads_k, P.R.D));
   MST_TRY(check_ld(ldo, heads_q, heads_k, P.R.D));
   if (misaligned(Q) || misaligned(K) || misaligned(Q_out) || misaligned(K_out)) return MST_ERR_SHAPE;
@@ -421,7 +421,7 @@ extern "C" mst_status_t mst_qk_norm_rotate_bwd(const mst_rotation_t* rotation, m
   MST_TRY(check_rows(dtype, tokens, seq_len, positions, heads_q, heads_k));
   if (heads_q == 0) Q = dQ_out = dQ = nullptr;       // a side without heads has no pointers
   if (heads_k == 0) K = dK_out = dK = nullptr;
-  if ((heads_q > 0 && (!dQ_out || !dQ || (P.R.gamma_q && !Q))) || (heads_k > 0 && (!dK_out || !dK || (P.R.gamma_k && !K))))
+  if (tokens > 0 && ((heads_q > 0 && (!dQ_out || !dQ || (P.R.gamma_q && !Q))) || (heads_k > 0 && (!dK_out || !dK || (P.R.gamma_k && !K)))))
     return MST_ERR_INVALID_ARG;
   if ((dgamma_q && !P.R.gamma_q) || (dgamma_k && !P.R.gamma_k)) return MST_ERR_INVALID_ARG;
   MST_TRY(check_ld(ld, heads_q, heads_k, P.R.D));
@@ -469,7 +469,7 @@ extern "C" mst_status_t mst_paged_append(const mst_paged_cache_t* cache, const m
   }
   if (!Q && !Q_out) heads_q = 0;
   if (heads_q == 0) Q = Q_out = nullptr;
-  if (heads_q < 0 || !K || !V || (heads_q > 0 && (!Q || !Q_out))) return MST_ERR_INVALID_ARG;
+  if (heads_q < 0 || (P.batch.tokens > 0 && (!K || !V || (heads_q > 0 && (!Q || !Q_out))))) return MST_ERR_INVALID_ARG;
   if (heads_q > 65535) return MST_ERR_SHAPE;
   MST_TRY(check_ld(ld, heads_q, cache->kv_heads, P.R.D));
   if (heads_q > 0) MST_TRY(check_ld(ldq, heads_q, 0, P.R.D));

@@ -259,3 +259,14 @@ def test_no_tokens_gives_zero_weight_gradients():
     mst.mst_qk_norm_rotate_bwd(c.rotation, 1, 0, 1, None, 2, 2, t, t, 256, t, t, 256, t, t, 256, *dg, ws)
     torch.cuda.synchronize()
     assert not dg[0].any() and not dg[1].any()
+
+
+def test_no_tokens_and_empty_tensors():
+    c = Case(0, 2, 2, 64, 64)
+    e = torch.empty((0, 256), dtype=torch.bfloat16, device=dev())
+    dg = [torch.ones(64, device=dev()), torch.ones(64, device=dev())]
+    ws = torch.empty(mst.mst_qk_norm_rotate_bwd_workspace(c.rotation, 0), dtype=torch.uint8, device=dev())
+    mst.mst_qk_norm_rotate_fwd(c.rotation, 1, 0, 1, None, 2, 2, e, e, 256, e, e, 256)
+    mst.mst_qk_norm_rotate_bwd(c.rotation, 1, 0, 1, None, 2, 2, e, e, 256, e, e, 256, e, e, 256, *dg, ws)
+    torch.cuda.synchronize()
+    assert not dg[0].any() and not dg[1].any()

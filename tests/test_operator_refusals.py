@@ -247,3 +247,17 @@ def test_orders_that_are_no_overlap(mst, kw):
 def test_append_of_keys_and_values_to_one_place(mst):
     assert _status(mst, _append, mst, cache=_cache(mst, K=A, V=A)) == INVALID
     _append(mst, cache=_cache(mst, K=A, V=A), batch=_batch(mst, tokens=0))
+
+
+def test_rows_of_no_tokens_have_no_address(mst):
+    """An empty tensor's address is NULL: a step without tokens is no wrong argument, as in the products."""
+    none = _batch(mst, tokens=0)
+    _fwd(mst, tokens=0, Q=None, K=None, Qo=None, Ko=None)
+    _bwd(mst, tokens=0, Q=None, K=None, dQo=None, dKo=None, dQ=None, dK=None, gq=None, gk=None)
+    _append(mst, batch=none, Q=None, K=None, V=None, Qo=None)
+    _append(mst, batch=none, K=None, V=None)
+    _attend(mst, batch=none, Q=None, Out=None, lse=None, ws=None, ws_bytes=0)
+    q = torch.empty((0, 128), dtype=torch.bfloat16)
+    mst.mst_paged_attention(_cache(mst), none, 2, 64, q, q.stride(0), q, q.stride(0), torch.empty((2, 0)), torch.empty(0), stream=0)
+    for f, kw in ((_fwd, dict(tokens=0, ld=100, Q=None)), (_append, dict(batch=none, ld=100, K=None)), (_attend, dict(batch=none, ldq=100, Q=None))):
+        assert _status(mst, f, mst, **kw) == SHAPE
