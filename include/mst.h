@@ -215,8 +215,8 @@ mst_status_t mst_strided_attention_bwd(const void* Q, const void* K, const void*
  *   rot_dim      a multiple of 16 up to head_dim; 0: no rotation (inv_freq may be NULL)
  *   inv_freq     device float [rot_dim / 2], in radians per position
  *   gamma_q, gamma_k   device float [head_dim], each NULL or 16-byte aligned; eps >= 0
- * Sums, norms and the turn are fp32, an angle is formed and reduced in fp64 (positions far out keep it to 2e-7); one rounding, at
- * the end. */
+ * Sums, norms and the turn are fp32; an angle loses its whole turns before it is rounded to fp32 and is right to 1e-7 at every position, for any
+ * |inv_freq| up to 2^40.  One rounding, at the end. */
 typedef struct {
   int32_t head_dim, rot_dim, interleaved;
   float eps;

@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
   }
   const float* gamma = is_q ? P.R.gamma_q : P.R.gamma_k;
   const Pairs<N> g = weights<INTER, N>(gamma, L);
-  const Frequencies F(P.R, lane);
+  const Frequencies<G, N> F(P.R, lane);
   int pos;
   mst_paged::Slot slot = {true, 0};
   if (APPEND) {
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) rotate_rows_kernel(const __grid
     const bool writes = !to_cache || slot.exists;
     Pairs<N> A, B;      // what u (A) and v (B) are multiplied by: A.u, B.u for u', A.v, B.v for v'
     {
-      const Turn<N> turn = turn_of<INTER, N>(tables[warp], P.R, F, L, pos, lane);
+      const Turn<N> turn = turn_of<INTER>(tables[warp], P.R, Steps<G, N>(F), L, pos, lane);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         A.u[k] = mul2(g.u[k], turn.c[k]);
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_ke
   const bool norm = gamma != nullptr, alone = !L.turns;
   const float inv_d = 1.f / (float)P.R.D;
   const Pairs<N> g = weights<INTER, N>(gamma, L);
-  const Frequencies F(P.R, lane);
+  const Steps<G, N> steps{Frequencies<G, N>(P.R, lane)};
   Pairs<N> acc = {};
   const unsigned groups = ((unsigned)P.tokens + WARPS - 1) / WARPS, all = groups * (unsigned)P.share;
   for (unsigned unit = blockIdx.x; unit < all; unit += gridDim.x) {
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(32 * WARPS, GRAD_BLOCKS_PER_SM) rotate_grad_ke
       no_row(ry[u]);
       fetch(begin + u, rx[u], ry[u]);
     }
-    const Turn<N> turn = turn_of<INTER, N>(tables[warp], P.R, F, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
+    const Turn<N> turn = turn_of<INTER>(tables[warp], P.R, steps, L, P.positions ? P.positions[token] : (int)((unsigned)token % (unsigned)P.seq_len), lane);
     for (int i0 = begin; i0 < end; i0 += AHEAD) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {

@@ -11,6 +11,7 @@
 #pragma once
 #include <cuda_bf16.h>
 
+#include "mst_angle.h"
 #include "mst_internal.cuh"
 #include "mst_tc_gemm.cuh"
 #include "mst_tc_ptx.cuh"
@@ -209,29 +210,43 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 // ---------------------------------------------------------------------------------------------- the turn
-// Cosines and sines of a position into a warp's own table, and out of it those of the lane's pairs.  The angle in turns, position * inv_freq /
-// 2 pi, is formed in fp64 and loses its whole part there: 53 bits hold 2^31 turns to 2^-22, and what is left goes to sincospi in fp32.
-// A lane keeps the frequencies that it sees to: lane, lane + 32, .. of rot / 2.
+// Cosines and sines of a position into a warp's own table, and out of it those of the lane's pairs.  An angle loses its whole turns before it is
+// rounded (mst_angle.h); what is left goes to sincospi in fp32, off by 2^-25 of half a turn at most: 1e-7.
+// A lane keeps the frequencies that it sees to: lane, lane + 32, .. of rot / 2; K of them are enough for the longest row of G lanes.
+template <int G, int N>
 struct Frequencies {
-  float f[MAX_HALF / 32];
+  static constexpr int K = 2 * G * N <= 32 ? 1 : 2 * G * N / 32;
+  float f[K];
   __device__ __forceinline__ Frequencies(const Rotation& R, int lane) {
 #pragma unroll
-    for (int k = 0; k < MAX_HALF / 32; ++k) f[k] = lane + 32 * k < R.rot / 2 ? R.inv_freq[lane + 32 * k] : 0.f;
+    for (int k = 0; k < K; ++k) f[k] = lane + 32 * k < R.rot / 2 ? R.inv_freq[lane + 32 * k] : 0.f;
+  }
+};
+// for all positions: made where nothing else is to be asked of memory any more (ahead of the lookup of rows to append 3 % of their time)
+template <int G, int N>
+struct Steps {
+  uint64_t step[Frequencies<G, N>::K];
+  uint32_t none = 0;          // bits: frequencies that are no finite numbers
+  __device__ __forceinline__ explicit Steps(const Frequencies<G, N>& F) {
+#pragma unroll
+    for (int k = 0; k < Frequencies<G, N>::K; ++k) {
+      step[k] = step_of(F.f[k]);
+      if (!(F.f[k] - F.f[k] == 0.f)) none |= 1u << k;
+    }
   }
 };
 template <int N>
 struct Turn {
   uint64_t c[N], s[N];
 };
-template <bool INTER, int N>
-__device__ __forceinline__ Turn<N> turn_of(float2* table, const Rotation& R, const Frequencies& F, const Lane& L, int pos, int lane) {
+template <bool INTER, int G, int N>
+__device__ __forceinline__ Turn<N> turn_of(float2* table, const Rotation& R, const Steps<G, N>& S, const Lane& L, int pos, int lane) {
   __syncwarp();
 #pragma unroll
-  for (int k = 0; k < MAX_HALF / 32; ++k) {
+  for (int k = 0; k < Frequencies<G, N>::K; ++k) {
     if (32 * k >= R.rot / 2) break;
-    const double turns = (double)pos * ((double)F.f[k] * 0.15915494309189533577);
     float2 v;
-    sincospif((float)(2.0 * (turns - rint(turns))), &v.y, &v.x);
+    sincospif((S.none >> k) & 1u ? NAN : half_turns(S.step[k], pos), &v.y, &v.x);
     table[lane + 32 * k] = v;
   }
   __syncwarp();

@@ -270,3 +270,51 @@ def test_no_tokens_and_empty_tensors():
     mst.mst_qk_norm_rotate_bwd(c.rotation, 1, 0, 1, None, 2, 2, e, e, 256, e, e, 256, e, e, 256, *dg, ws)
     torch.cuda.synchronize()
     assert not dg[0].any() and not dg[1].any()
+
+
+@pytest.mark.parametrize("top", [1.0, 1000.0])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_at_every_position(interleaved, top):
+    """Pairs (1, 0): the results are cosines and sines themselves, nothing else is rounded.  The angle is rounded to fp32 as a number of half turns of
+    at most 1 (2^-25 of half a turn, 9.4e-8), sincospi's results by up to 2 units of 2^-24 (1.2e-7): 2.2e-7."""
+    from test_angle import INV_TWO_PI, BITS
+    from fractions import Fraction
+    T, D = 400, 256
+    c = Case(T, 1, 1, D, D, interleaved, dtype="f32", norm="", first=0)
+    g = torch.Generator().manual_seed(5)
+    pos = torch.randint(-(1 << 31), (1 << 31) - 1, (T,), generator=g)
+    pos[::3] = (1 << 31) - 1 - torch.randint(0, 1 << 20, pos[::3].shape, generator=g)
+    pos[:4] = torch.tensor([0, 1, (1 << 31) - 1, -(1 << 31)])
+    c.positions = pos.to(torch.int32).to(dev())
+    f = (top * 10000.0 ** (-torch.arange(D // 2, dtype=torch.float64) / (D // 2) * torch.rand(1, generator=g).item())).float()
+    c.dev_freq.copy_(f)
+    x = torch.zeros(T, 2, D)
+    x[..., slice(0, D, 2) if interleaved else slice(0, D // 2)] = 1.0
+    x = x.view(T, 2 * D)
+    y, dx = c.padded(), c.padded()
+    c.forward(c.padded(x), y)
+    c.backward(c.padded(x), c.padded(x), dx)
+    torch.cuda.synchronize()
+    # pos * f / 2 pi in whole numbers: f is a 24-bit number times a power of two
+    angle = np.empty((T, D // 2))
+    for i, fi in enumerate(f.tolist()):
+        n, d = Fraction(fi).as_integer_ratio()
+        for t, p in enumerate(pos.tolist()):
+            angle[t, i] = 2 * np.pi * ((((p * n * INV_TWO_PI) // d) >> (BITS - 80)) % (1 << 80)) * 2.0 ** -80
+    for got, sign in ((y, 1.0), (dx, -1.0)):
+        h = host(got).astype(np.float64).reshape(T, 2, D)
+        a, b = (h[..., 0::2], h[..., 1::2]) if interleaved else (h[..., : D // 2], h[..., D // 2:])
+        assert np.abs(a - np.cos(angle)[:, None]).max() <= 2.2e-7
+        assert np.abs(b - sign * np.sin(angle)[:, None]).max() <= 2.2e-7
+
+
+def test_frequencies_that_are_no_numbers():
+    c = Case(5, 2, 1, 64, 64, norm="", dtype="f32", first=0)
+    c.dev_freq[3], c.dev_freq[30] = float("inf"), float("nan")
+    y, dx = c.padded(), c.padded()
+    c.forward(c.padded(c.x), y)
+    c.backward(c.padded(c.x), c.padded(c.dy), dx)
+    torch.cuda.synchronize()
+    for t in (y, dx):
+        h = host(t).reshape(5, 3, 2, 32)
+        assert np.isnan(h[..., [3, 30]]).all() and np.isfinite(np.delete(h, [3, 30], -1)).all()
