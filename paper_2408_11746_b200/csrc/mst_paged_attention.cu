@@ -394,6 +394,7 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
 constexpr int TILE_ROWS = 128, FEW_ROWS = 16;
 constexpr double TILES_FROM = 250e3, TILES_FROM_STRIDED = 900e3;
 constexpr int64_t MOST_STEPS = 1 << 18;
+constexpr int MOST_PAGES = 1 << 27;
 Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, int stride) {
   Plan p;
   const int group = heads / c.kv_heads;
@@ -405,9 +406,10 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
     return stride >= len || nt >= stride ? len : (stride + nt < len ? stride + nt : len) + len / stride * nt;
   };
   const bool strided = len / 2 >= stride && stride >= DENSE_BELOW;
-  // A tile's strided keys are formed ahead of its first products, which some of its warps wait for, 0.8 s at least and not for ever: 2^18 of them take 0.4
+  // What a tile does ahead of its first products some of its warps wait for, 0.8 s at least and not for ever: 2^18 strided keys take 0.4, to look through 2^27
+  // pages for those that do not exist, 256 at a time, as long
   const int64_t reach = (int64_t)b.table_stride * c.page_size;
-  p.tiles = rows > FEW_ROWS && group <= TILE_ROWS && (stride < DENSE_BELOW || reach / stride < MOST_STEPS) &&
+  p.tiles = rows > FEW_ROWS && group <= TILE_ROWS && b.table_stride < MOST_PAGES && (stride < DENSE_BELOW || reach / stride < MOST_STEPS) &&
             (double)lists * (double)((rows + FEW_ROWS - 1) / FEW_ROWS) * (double)entries(FEW_ROWS) >= (strided ? TILES_FROM_STRIDED : TILES_FROM);
   p.rows = p.tiles ? TILE_ROWS / group * group : rows <= FEW_ROWS / 2 ? FEW_ROWS / 2 : FEW_ROWS;
   const int64_t tiles = (rows + p.rows - 1) / p.rows;

@@ -261,3 +261,10 @@ def test_rows_of_no_tokens_have_no_address(mst):
     mst.mst_paged_attention(_cache(mst), none, 2, 64, q, q.stride(0), q, q.stride(0), torch.empty((2, 0)), torch.empty(0), stream=0)
     for f, kw in ((_fwd, dict(tokens=0, ld=100, Q=None)), (_append, dict(batch=none, ld=100, K=None)), (_attend, dict(batch=none, ldq=100, Q=None))):
         assert _status(mst, f, mst, **kw) == SHAPE
+
+
+def test_form_of_the_attention_with_very_many_pages(mst):
+    """A table with room for 2^27 pages of a sequence or more: few rows."""
+    for table, splits in (((1 << 27) - 1, 5), (1 << 27, 2), ((1 << 31) - 1, 2)):
+        b = _batch(mst, tokens=1000, max_new=800, max_len=20000, table_stride=table)
+        assert mst.mst_paged_attention_workspace(_cache(mst), b, 4, 1 << 30) == splits * 1000 * 4 * 66 * 4
