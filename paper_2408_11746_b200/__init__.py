@@ -321,9 +321,16 @@ def _bytes(workspace) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
+def _positions(positions, tokens: int) -> Optional[int]:
+    if hasattr(positions, "data_ptr") and (str(positions.dtype) != "torch.int32" or positions.dim() != 1 or positions.shape[0] < tokens or
+                                           not positions.is_contiguous()):
+        raise ValueError("positions [tokens] is a contiguous int32 tensor")
+    return _ptr(positions)
+
+
 def mst_qk_norm_rotate_fwd(rotation: Rotation, dtype: int, tokens: int, seq_len: int, positions, heads_q: int, heads_k: int, Q, K,
                            ld: int, Q_out, K_out, ldo: int, stream=None) -> None:
-    _check(_lib.mst_qk_norm_rotate_fwd(rotation, dtype, tokens, seq_len, _ptr(positions), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
+    _check(_lib.mst_qk_norm_rotate_fwd(rotation, dtype, tokens, seq_len, _positions(positions, tokens), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
                                        _ptr(Q_out), _ptr(K_out), ldo, _stream(stream)), "mst_qk_norm_rotate_fwd")
 
 
@@ -337,7 +344,7 @@ def mst_qk_norm_rotate_bwd(rotation: Rotation, dtype: int, tokens: int, seq_len:
                            ld: int, dQ_out, dK_out, lddo: int, dQ, dK, ldg: int, dgamma_q=None, dgamma_k=None, workspace=None,
                            stream=None) -> None:
     """workspace: a tensor of at least ``mst_qk_norm_rotate_bwd_workspace`` bytes."""
-    _check(_lib.mst_qk_norm_rotate_bwd(rotation, dtype, tokens, seq_len, _ptr(positions), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
+    _check(_lib.mst_qk_norm_rotate_bwd(rotation, dtype, tokens, seq_len, _positions(positions, tokens), heads_q, heads_k, _ptr(Q), _ptr(K), ld,
                                        _ptr(dQ_out), _ptr(dK_out), lddo, _ptr(dQ), _ptr(dK), ldg, _ptr(dgamma_q), _ptr(dgamma_k),
                                        _ptr(workspace), _bytes(workspace), _stream(stream)), "mst_qk_norm_rotate_bwd")
 

@@ -268,3 +268,15 @@ def test_form_of_the_attention_with_very_many_pages(mst):
     for table, splits in (((1 << 27) - 1, 5), (1 << 27, 2), ((1 << 31) - 1, 2)):
         b = _batch(mst, tokens=1000, max_new=800, max_len=20000, table_stride=table)
         assert mst.mst_paged_attention_workspace(_cache(mst), b, 4, 1 << 30) == splits * 1000 * 4 * 66 * 4
+
+
+def test_positions_check_their_type(mst):
+    """arange's own type is int64: read as int32, every other position would be 0."""
+    p = torch.arange(8)
+    for bad in (p, p.float(), p.int()[::2], p.int().view(2, 4), p.int()[:3]):
+        with pytest.raises(ValueError):
+            _fwd(mst, tokens=4, positions=bad)
+        with pytest.raises(ValueError):
+            mst.mst_qk_norm_rotate_bwd(_rot(mst), 1, 4, 4, bad, 2, 2, A, A, 128, A, A, 128, A, A, 128, stream=0)
+    _fwd(mst, tokens=0, positions=p.int()[:0])
+    assert _status(mst, _fwd, mst, tokens=4, positions=p.int(), dtype=9) == DTYPE       # further checks are the library's
