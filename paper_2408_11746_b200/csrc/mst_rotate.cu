@@ -359,7 +359,7 @@ mst_status_t launch_grad(GradParams& P, float* dgamma_q, float* dgamma_k, cudaSt
 
 // counts and types that the training calls have in common
 mst_status_t check_rows(mst_dtype_t dtype, int64_t tokens, int32_t seq_len, const int32_t* positions, int32_t hq, int32_t hk) {
-  if (tokens < 0 || hq < 0 || hk < 0 || (!positions && seq_len <= 0)) return MST_ERR_INVALID_ARG;
+  if (tokens < 0 || hq < 0 || hk < 0 || (tokens > 0 && !positions && seq_len <= 0)) return MST_ERR_INVALID_ARG;
   if (dtype != MST_F32 && dtype != MST_BF16) return MST_ERR_DTYPE;
   if (tokens > 0x7FFFFFFF || hq > 65535 || hk > 65535) return MST_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return MST_ERR_SHAPE;

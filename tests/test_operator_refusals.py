@@ -280,3 +280,9 @@ def test_positions_check_their_type(mst):
             mst.mst_qk_norm_rotate_bwd(_rot(mst), 1, 4, 4, bad, 2, 2, A, A, 128, A, A, 128, A, A, 128, stream=0)
     _fwd(mst, tokens=0, positions=p.int()[:0])
     assert _status(mst, _fwd, mst, tokens=4, positions=p.int(), dtype=9) == DTYPE       # further checks are the library's
+
+
+def test_positions_of_no_tokens_have_no_address(mst):
+    none = torch.empty(0, dtype=torch.int32)
+    _fwd(mst, tokens=0, seq=0, positions=none, Q=None, K=None, Qo=None, Ko=None)
+    mst.mst_qk_norm_rotate_bwd(_rot(mst), 1, 0, 0, none, 2, 2, None, None, 128, None, None, 128, None, None, 128, stream=0)
