@@ -215,7 +215,7 @@ mst_status_t mst_strided_attention_bwd(const void* Q, const void* K, const void*
  *   rot_dim      a multiple of 16 up to head_dim; 0: no rotation (inv_freq may be NULL)
  *   inv_freq     device float [rot_dim / 2], in radians per position
  *   gamma_q, gamma_k   device float [head_dim], each NULL or 16-byte aligned; eps >= 0
- * Sums, norms and the turn are fp32; an angle loses its whole turns before it is rounded to fp32 and is right to 1e-7 at every position, for any
+ * Sums, norms and the turn are fp32 (a row's x^2 add up to less than 3e38); an angle loses its whole turns before it is rounded to fp32 and is right to 1e-7 at every position, for any
  * |inv_freq| up to 2^40.  One rounding, at the end. */
 typedef struct {
   int32_t head_dim, rot_dim, interleaved;

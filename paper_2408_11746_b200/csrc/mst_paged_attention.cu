@@ -387,10 +387,14 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const __grid_constant__
 // ---------------------------------------------------------------------------------------------- the call
 // Which form, by what the few-row form would go through: entries of its lists, over all 16-row tiles.  Up to 16 rows it always serves (12 heads, 3000
 // positions, 16 new tokens of 32 sequences 70 us, in 128-row tiles 86); beyond, a list that fills eight such tiles is better walked once.  Measured with 24 to
-// 96 new tokens of 1, 8 and 32 sequences, few rows / tiles in us: every position attended 13.5 / 22 (72 thousand entries), 15 / 23 (144), 22 / 24 (216),
-// 38 / 29 (576), 88 / 86 (2304); stride 256, where tiles form a strided key for each row, 13 / 22 (86), 25 / 35 (257), 50 / 64 (515), 69 / 75 (686),
-// 94 / 81 (1030); 4 x 512 tokens over 8192, stride 256 78 / 85 (1178), stride 1024 89 / 65 (1768), 4 x 2048 tokens, stride 256 255 / 160 (4712).
+// 96 new tokens of 1, 8 and 32 sequences over 3000 positions, 12 heads, few rows / tiles in us: every position attended 14 / 23 (72 thousand entries),
+// 22 / 24 (216), 39 / 29 (576), 45 / 31 (864), 88 / 86 (2304); stride 256, where tiles form a strided key for each row, 13 / 22 (86), 25 / 34 (258),
+// 50 / 67 (516), 94 / 81 (1032); 4 x 512 tokens over 8192, stride 1024 89 / 43 (1790), stride 256 94 / 86 (1200), 4 x 2048 tokens 329 / 223.
 // (A few-row form of 32 rows lost to the one of 16 in all of them.)
+// The count of entries is not all: where strides are short against the lists, tiles form far more strided keys than they have tiles to cut a list by
+// (TileWalk::range), and the rule takes them all the same.  Stride 64: 4 x 512 over 8192 222 / 306, 12 heads, 1024 tokens over 32768 429 / 606, and with 4
+// heads, 512 tokens 98 / 560; stride 128, 20 heads on 4, 2 x 1024 over 16384 135 / 254; 128 columns, stride 256, 4 x 512 over 8192 129 / 163, 32 x 96 over 3000
+// 117 / 122; strides below 64, whose masks tiles work out key by key, 4 x 512 over 2048 to 8192 stride 32 273 / 1091, stride 2 848 / 1102.
 constexpr int TILE_ROWS = 128, FEW_ROWS = 16;
 constexpr double TILES_FROM = 250e3, TILES_FROM_STRIDED = 900e3;
 constexpr int64_t MOST_STEPS = 1 << 18;
@@ -414,8 +418,10 @@ Plan plan_of(const mst_paged_cache_t& c, const mst_paged_batch_t& b, int heads, 
   p.rows = p.tiles ? TILE_ROWS / group * group : rows <= FEW_ROWS / 2 ? FEW_ROWS / 2 : FEW_ROWS;
   const int64_t tiles = (rows + p.rows - 1) / p.rows;
   p.count = (int)(tiles < 65535 ? tiles : 65535);
-  // Long lists are cut into ranges until there are blocks for the whole GPU, two of which an SM holds.  Tiles: for one wave and no more (432 blocks of up to
-  // 94 tiles: cut into 960 9 us more, when it took 272).  Few rows: for two, as lists are of many lengths (long ragged contexts 41.8 us, for six waves 47.9).
+  // Long lists are cut into ranges until there are blocks for the whole GPU, two of which an SM holds.  Tiles: no more than one wave (432 blocks of up to
+  // 94 tiles: cut into 960 9 us more, when it took 272); at 128 columns, where an SM holds one block, that is two waves, which pays for lists of several lengths (300
+  // to 900 new tokens over 2000 to 16000 positions, 8 heads, 99 us, for one wave 181; 1024 over 16384, 12 heads, 140 and 173) and costs where they are alike (1536
+  // over 16384, 12 heads, 193 and 169; 128 over 32768, 8 heads, 54 and 42).  Few rows: for two, as lists are of many lengths (long ragged contexts 41.8 us, for six waves 47.9).
   // units: tiles of 128 keys and strided keys, which take about as long; or 64 entries
   int64_t units, want = 2 * (int64_t)mst_sm_count();
   if (p.tiles) {

@@ -146,7 +146,8 @@ struct TileWalk {
     far = dense || T.p_hi / 2 < T.l ? 0 : T.p_hi / T.l - m_first + 1;
   }
   // Range `split` of at most `splits` equal ranges, each with `least` tiles and steps or more and a near tile: near tiles n0 .. n1 - 1, strided keys
-  // m0 .. m1 - 1 steps behind.  active: how many ranges there are.
+  // m0 .. m1 - 1 steps behind.  active: how many ranges there are; with short strides over long contexts fewer than are planned for (two or three near
+  // tiles and hundreds of steps: the blocks and the workspace of the others are not used).
   MST_HD bool range(int splits, int least, int split, int& n0, int& n1, int& m0, int& m1, int& active) const {
     const int64_t parts = ((int64_t)near + far + least - 1) / least;
     active = (int)(parts < splits ? parts : splits);

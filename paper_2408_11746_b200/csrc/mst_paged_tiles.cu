@@ -565,6 +565,7 @@ paged_tiles_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
           uint32_t seen[2] = {there[0], there[1]};      // this row's keys
           if (some_not) {
             if (MODE == DENSE) {
+              // 64 remainders a thread, which is what takes the time: 4 x 512 tokens over 2048 to 8192, 12 heads, 1.1 ms (every position 0.12)
 #pragma unroll 1
               for (int e = 0; e < 64; ++e)
                 if (!near_sees(P.l, pos, k0 + e)) seen[e >> 5] &= ~(1u << (e & 31));

@@ -1,8 +1,11 @@
 // Norm of queries and keys for each head with the position rotation in the same pass: forward, gradients, and the form that
 // appends to a paged cache.  The arithmetic of a row is in mst_rotate.cuh; the kernels differ in where rows come from and go to.
 //
-// Bound: HBM (each row is read once and written once), or a launch and a trip to memory where there are few tokens.  A warp takes a token (or
-// a share of its heads) and has the loads of its first steps in flight before it works out the angles; no block-wide step on the way.
+// Each row is read once and written once.  A warp takes a token (or a share of its heads) and has the loads of its first steps in flight before it works
+// out the angles; no block-wide step on the way.
+// Bound: latency.  124 registers leave 16 warps an SM, each with three rows in flight, and a warp's instructions wait: forward (16384 tokens of 24 rows of
+// 64, 24 us, 725 instructions a token) a quarter of the time for memory, a fifth for the instruction before, a tenth for shared memory, with issue slots 52 % busy
+// and DRAM 29; gradients (40 rows, 56 us) a fifth for memory, a quarter for the instruction before, 57 % and 50.  Few tokens: a launch and a trip to memory.
 #include "mst_paged.cuh"
 #include "mst_rotate.cuh"
 
